@@ -289,6 +289,111 @@ int mlkv_read_rows(mlkv_table *t, const int64_t *d_rows, int64_t n, float *d_row
  * 0xFFFFFFFF and makes the next mlkv_sync return MLKV_EINVAL. */
 int mlkv_read_staleness(mlkv_table *t, const int64_t *d_rows, int64_t n, uint32_t *d_out, void *hip_stream);
 
+/* ---- the dense operators of a training step ----
+ * What a step computes between the get of its rows and the put_grad of their
+ * gradients (workflow steps 3 to 7, Sec. III-B), as far as it is row-wise, and
+ * the update of the weights that no table holds. They need no table: every
+ * buffer is the caller's, on the current HIP device, and hip_stream is a
+ * stream of that device. Nothing is allocated and nothing kept, so any of them
+ * may be recorded into a HIP graph, and calls on different streams do not
+ * disturb each other as long as their buffers differ (workspaces included).
+ * Rows lie `*_stride` ELEMENTS apart (>= the row's length, or 0 in an input
+ * whose rows are all the same; any alignment of the element type), the elements of a
+ * row next to each other. Arguments are checked before anything is launched:
+ * MLKV_EINVAL leaves every buffer as it was. Equal calls give equal bits. */
+
+/* Element types of the calls below. */
+enum { MLKV_F32 = 0, MLKV_BF16 = 1, MLKV_F16 = 2 };
+
+/* Layer norm of n rows of dim elements:
+ *     mu = mean(x), v = mean((x - mu)^2)       (held in fp32 and corrected for
+ *                                               mu's rounding)
+ *     out[c] = (x[c] - mu) / sqrt(v + eps) * weight[c] + bias[c]
+ * rounded once to the type of x. d_weight, d_bias: dim elements of type
+ * weight_dtype (MLKV_F32 or dtype), either may be NULL (1, 0). d_out may be d_x
+ * (with the same stride). 0 <= n <= 2^31 - 1, 1 <= dim <= MLKV_NORM_MAX_DIM,
+ * eps >= 0 and finite; with eps = 0 a row of equal elements gives NaN. */
+#define MLKV_NORM_MAX_DIM 16384
+int mlkv_layer_norm(const void *d_x, int64_t x_stride, const void *d_weight, const void *d_bias, int64_t n,
+                    int32_t dim, float eps, int dtype, int weight_dtype, void *d_out, int64_t out_stride,
+                    void *hip_stream);
+
+/* Its gradient: with d_grad the gradient of its output, r = 1 / sqrt(v + eps),
+ * h = (x - mu) * r and g = grad * weight,
+ *     d_x_grad[c]    = r * (g[c] - mean(g) - h[c] * mean(g * h))
+ *     weight_grad[c] = sum over rows of grad[c] * h[c]
+ *     bias_grad[c]   = sum over rows of grad[c]
+ * mu and v are taken from x again. x, grad and x_grad are of type dtype (fp32
+ * rows of x_grad are what mlkv_put_grad takes), weight, weight_grad and
+ * bias_grad of weight_dtype. The sums over rows are fp32 within a block of
+ * rows and fp64 over the blocks, in a fixed order; with n = 0 they are 0.
+ * d_weight may be NULL (1); d_x_grad, d_weight_grad and d_bias_grad may each
+ * be NULL (not wanted). d_x_grad may be d_grad or d_x (same stride). d_work:
+ * mlkv_layer_norm_grad_workspace(n, dim) bytes at a multiple of 16 (may be
+ * NULL where neither sum is wanted). Limits as mlkv_layer_norm. */
+int64_t mlkv_layer_norm_grad_workspace(int64_t n, int32_t dim);
+int mlkv_layer_norm_grad(const void *d_x, int64_t x_stride, const void *d_weight, const void *d_grad,
+                         int64_t grad_stride, int64_t n, int32_t dim, float eps, int dtype, int weight_dtype,
+                         void *d_x_grad, int64_t x_grad_stride, void *d_weight_grad, void *d_bias_grad, void *d_work,
+                         int64_t work_bytes, void *hip_stream);
+
+/* Log probabilities under n rows of vocab logits x, one given token a row:
+ *     m = max(x), s = sum exp(x - m), log p[j] = x[j] - m - log(s)
+ *     d_logp[i]     = log p[tokens[i]]
+ *     d_entropy[i]  = - sum p[j] log p[j]
+ *     d_stats[i]    = { m, log(s) }  (2 floats; their sum is the log of the sum
+ *                     of exponentials, apart so that no digits are lost)
+ *     d_top_ids[i*top ...]  = the `top` largest logits' indices, largest first,
+ *                     equal ones lowest index first; d_top_logp their log p
+ * The sums are fp32 a thread, joined in a fixed order. A token < 0 marks a
+ * position without one: its logp is 0. A token >= vocab gives NaN. A logit of
+ * -inf has probability 0; a row of nothing else has no distribution: logp and
+ * top_logp -inf, entropy 0, stats { -inf, 0 }, ids 0, 1, ... A NaN or +inf in a
+ * row makes its outputs NaN (logp 0 still where it has no token) and its ids -1.
+ * d_logp needs d_tokens; d_logp, d_entropy, d_stats may be NULL (not wanted),
+ * and d_top_ids, d_top_logp must be NULL where top is 0 (either may be NULL
+ * otherwise). 0 <= n <= 2^31 - 1, 1 <= vocab <= MLKV_LOGITS_MAX_VOCAB,
+ * 0 <= top <= min(vocab, MLKV_LOGITS_MAX_TOP). d_work:
+ * mlkv_log_probs_workspace(n, vocab, top, dtype) bytes at a multiple of 16. */
+#define MLKV_LOGITS_MAX_VOCAB 16777216
+#define MLKV_LOGITS_MAX_TOP 64
+int64_t mlkv_log_probs_workspace(int64_t n, int64_t vocab, int32_t top, int dtype);
+int mlkv_log_probs(const void *d_logits, int64_t stride, const int64_t *d_tokens, int64_t n, int64_t vocab,
+                   int32_t top, int dtype, float *d_logp, float *d_entropy, float *d_stats, int64_t *d_top_ids,
+                   float *d_top_logp, void *d_work, int64_t work_bytes, void *hip_stream);
+
+/* Gradient of those outputs in the logits: with a = d_logp_grad[i] (taken as 0
+ * at a token < 0), b = d_entropy_grad[i] and H the row's entropy,
+ *     d_logits_grad[j] = a * ((j == token) - p[j]) - b * p[j] * (log p[j] + H)
+ * where p comes from d_stats as mlkv_log_probs wrote it. d_logp_grad (with
+ * d_tokens) or d_entropy_grad (with d_entropy) may be NULL (0). A row without a
+ * distribution gets zeros, a token >= vocab NaN. d_logits_grad is of the
+ * logits' type and may be d_logits (same stride). Limits as mlkv_log_probs. */
+int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_tokens, const float *d_stats,
+                        const float *d_entropy, const float *d_logp_grad, const float *d_entropy_grad, int64_t n,
+                        int64_t vocab, int dtype, void *d_logits_grad, int64_t grad_stride, void *hip_stream);
+
+/* A dense weight's update made orthogonal by Newton-Schulz steps (the quintic
+ * iteration of the Muon optimiser): for each of `batch` matrices G,
+ *     X = G / (||G|| + eps)     (Frobenius norm; transposed where rows > cols)
+ *     `steps` times:  A = X X^T,  B = b A + c A^2,  X = a X + B X
+ *     out = X                   (transposed back)
+ * with (a, b, c) = (3.4445, -4.7750, 2.0315). The norm is summed in fp64; X, A
+ * and B are held as pairs of fp16 numbers (22 bits of an element, but none
+ * below 2^-40, so that an update whose norm is far below eps loses digits) and
+ * their products are summed in fp32. G and out are of type dtype, row-major with rows *_stride
+ * and matrices *_batch_stride elements apart; out may be G itself (same strides).
+ * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.
+ * 0 <= batch <= 65535, 1 <= rows, cols <= MLKV_ORTH_MAX_DIM, 1 <= steps <= 64,
+ * eps > 0 and finite.
+ * d_work: mlkv_orthogonalize_workspace(batch, rows, cols) bytes at a multiple
+ * of 256. */
+#define MLKV_ORTH_MAX_DIM 32768
+int64_t mlkv_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols);
+int mlkv_orthogonalize(const void *d_g, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows,
+                       int64_t cols, int32_t steps, float eps, int dtype, void *d_out, int64_t out_batch_stride,
+                       int64_t out_row_stride, void *d_work, int64_t work_bytes, void *hip_stream);
+
 /* ---- per-kernel timing (benchmarks) ----
  * The library runs MLKV_NUM_KERNELS kernels: 0 get_probe_gather and
  * 1 assign_new for mlkv_get, mlkv_get_bounded and mlkv_lookahead (rows wider

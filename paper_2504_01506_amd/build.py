@@ -14,7 +14,8 @@ KERNELS = os.path.join(CSRC, "mlkv_kernels.hip")
 # the row maps of mlkv_kernels.h (MLKV_MAPS), one compilation of mlkv_kernels.hip each, the slowest first
 MAPS = ("MapD1024", "MapD512", "MapD256", "MapD128", "MapD64", "MapD32", "MapD16", "MapD3")
 UNITS = [(KERNELS, m) for m in MAPS] + [(os.path.join(CSRC, f), None)
-                                       for f in ("mlkv_kernels.hip", "mlkv_api.hip", "mlkv_tier.hip")]
+                                       for f in ("mlkv_kernels.hip", "mlkv_api.hip", "mlkv_tier.hip", "mlkv_norm.hip",
+                                                 "mlkv_logits.hip", "mlkv_orth.hip")]
 LIB = os.path.join(HERE, "libmlkv.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

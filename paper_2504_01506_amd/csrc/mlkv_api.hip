@@ -11,6 +11,7 @@
 
 #include "mlkv.h"
 #include "mlkv_kernels.h"
+#include "mlkv_ops.h"
 #include "mlkv_pool.h"
 
 using namespace mlkv;
@@ -373,6 +374,26 @@ extern "C" {
 const char* mlkv_last_error(void) { return g_err.c_str(); }
 
 }  // extern "C"
+
+namespace mlkv {
+
+int op_error(int code, const char* msg) noexcept {
+  try {
+    return fail(code, msg);
+  } catch (...) {  // (no memory for the text: the code still tells)
+    return code;
+  }
+}
+
+int op_launch_error(hipError_t e, const char* what) noexcept {
+  try {
+    return hip_fail(e, what);
+  } catch (...) {
+    return e == hipErrorOutOfMemory ? MLKV_ENOMEM : MLKV_EDEVICE;
+  }
+}
+
+}  // namespace mlkv
 
 namespace {
 

@@ -1,0 +1,72 @@
+// What the dense operators (mlkv_norm.hip, mlkv_logits.hip, mlkv_orth.hip)
+// share: element types, vectors of them, sums over lanes, host-side checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mlkv.h"
+
+namespace mlkv {
+
+// Set the calling thread's error text (mlkv_last_error) and return the code.
+int op_error(int code, const char* msg) noexcept;
+int op_launch_error(hipError_t e, const char* what) noexcept;
+
+using bf16 = __bf16;
+using f16 = _Float16;
+
+inline int dtype_size(int dtype) {
+  return dtype == MLKV_F32 ? 4 : dtype == MLKV_BF16 || dtype == MLKV_F16 ? 2 : 0;
+}
+
+// Calls f(T{}) with T the C++ type of dtype, which has been checked.
+template <class F>
+auto dispatch_type(int dtype, F f) {
+  if (dtype == MLKV_F32) return f(float{});
+  if (dtype == MLKV_BF16) return f(bf16{});
+  return f(f16{});
+}
+
+// Whether all of `ptrs`, and the strides in elements of `size` bytes, are multiples of `bytes`.
+inline bool all_aligned(size_t bytes, size_t size, std::initializer_list<const void*> ptrs,
+                        std::initializer_list<int64_t> strides) {
+  uintptr_t x = 0;
+  for (const void* p : ptrs) x |= reinterpret_cast<uintptr_t>(p);
+  for (int64_t s : strides) x |= static_cast<uintptr_t>(s) * size;
+  return x % bytes == 0;
+}
+
+// Whether `rows` rows of `width` elements `stride` apart are something an
+// input (same: stride 0 allowed) or an output can be: no rows that overlap,
+// and offsets in bytes within 63 bits.
+inline bool stride_ok(int64_t stride, int64_t rows, int64_t width, bool same) {
+  if (rows <= 1) return true;
+  if (same && stride == 0) return true;
+  return stride >= width && stride <= (int64_t(1) << 60) / rows;
+}
+
+// V elements of T as one load or store.
+template <class T, int V>
+struct __align__(sizeof(T) * V) Pack {
+  T v[V];
+};
+
+// The sum of v over groups of G lanes (a power of two, at most 64), in every
+// lane of the group. All lanes of the wave must be active. Within 16 lanes by
+// data-parallel moves (xor 1, xor 2, then mirrors, which meet equal values).
+template <int kCtrl>
+__device__ __forceinline__ float dpp_move(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float group_sum(float v, int G) {
+  if (G > 1) v += dpp_move<0xB1>(v);    // quad_perm 1 0 3 2
+  if (G > 2) v += dpp_move<0x4E>(v);    // quad_perm 2 3 0 1
+  if (G > 4) v += dpp_move<0x141>(v);   // row_half_mirror
+  if (G > 8) v += dpp_move<0x140>(v);   // row_mirror
+  if (G > 16) v += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x401F));  // xor 16
+  if (G > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
+}  // namespace mlkv

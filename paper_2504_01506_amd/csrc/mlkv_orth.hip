@@ -1,0 +1,423 @@
+// Updates made orthogonal by Newton-Schulz steps.
+//
+// Three products a step, all of the form C[i][j] = sum_k P[i][k] Q[j][k] with
+// both operands' k running in memory, as the matrix units want it: X X^T, then
+// A A (A is symmetric), then B X from X^T, which is kept beside X. The first
+// two results are symmetric: only tiles on and below the diagonal are computed,
+// and written twice.
+//
+// Numbers are held as fp16 pairs hi + lo, 22 bits: norms bound every entry
+// (|X| <= 1.21, |A| <= 1.45, |B| <= 2.81, the quintic's largest values), so one
+// power of two a matrix, 2^15 for X and A, 2^14 for B, keeps hi below 65504
+// and lo in its range. A product takes hi hi + hi lo + lo hi; what is left out
+// is 2^-22 of it, below the rounding of the fp32 sums. Bound by the matrix
+// units: three fp16 products instead of one fp32 product, at 16 times the rate.
+#include "mlkv_ops.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace mlkv {
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr int kThreads = 256;
+constexpr int kDepth = 32;       // k of a stage: 64 bytes a row and plane
+constexpr int kNormBlocks = 64;  // sums of squares a matrix
+
+using half4 = _Float16 __attribute__((ext_vector_type(4)));
+using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using float16v = float __attribute__((ext_vector_type(16)));
+
+struct Shape {
+  int m, n;    // as iterated on: m <= n
+  int mp, np;  // padded to whole tiles, zeros in the padding
+  bool turned; // rows > cols
+};
+
+struct User {
+  const void* g;
+  void* out;
+  int64_t g_batch, g_row, o_batch, o_row;
+};
+
+// ---- norm and first X ----
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_orth_norm(User u, int64_t rows, int64_t cols, double* sums) {
+  __shared__ double part[kThreads / 64];
+  const T* g = static_cast<const T*>(u.g) + blockIdx.y * u.g_batch;
+  double t = 0.0;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int64_t c = threadIdx.x; c < cols; c += kThreads) {
+      const double v = (double)(float)g[r * u.g_row + c];
+      t += v * v;
+    }
+  for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) sums[blockIdx.y * kNormBlocks + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+}
+
+__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
+  hi = (_Float16)v;
+  lo = (_Float16)(v - (float)hi);
+}
+
+// Planes of one matrix: hi at p, lo `plane` elements behind it.
+struct Planes {
+  _Float16* p;
+  int64_t plane, batch;
+  int ld;
+};
+
+// X and X^T from G, 64 x 64 elements a block, the transposed ones through LDS.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const double* sums, int nsums, float eps,
+                                                         Planes straight, Planes turned, int rows, int cols) {
+  __shared__ float tile[64][65];
+  double t = 0.0;
+  for (int k = 0; k < nsums; ++k) t += sums[blockIdx.z * kNormBlocks + k];
+  const double inv = 32768.0 / (sqrt(t) + (double)eps);
+  const T* g = static_cast<const T*>(u.g) + blockIdx.z * u.g_batch;
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  _Float16* a = straight.p + blockIdx.z * straight.batch;
+  for (int y = ty; y < 64; y += 4) {
+    const int r = r0 + y, c = c0 + tx;
+    const float v = r < rows && c < cols ? (float)((double)(float)g[r * u.g_row + c] * inv) : 0.0f;
+    tile[y][tx] = v;
+    _Float16 hi, lo;
+    split(v, hi, lo);
+    const int64_t at = (int64_t)r * straight.ld + c;
+    a[at] = hi;
+    a[straight.plane + at] = lo;
+  }
+  __syncthreads();
+  _Float16* b = turned.p + blockIdx.z * turned.batch;
+  for (int y = ty; y < 64; y += 4) {
+    _Float16 hi, lo;
+    split(tile[tx][y], hi, lo);
+    const int64_t at = (int64_t)(c0 + y) * turned.ld + r0 + tx;
+    b[at] = hi;
+    b[turned.plane + at] = lo;
+  }
+}
+
+// ---- products ----
+enum Step : int { kSquareX, kSquareA, kApplyB, kApplyLast };
+
+struct ProdArgs {
+  Planes P, Q;   // operands
+  Planes add;    // what the epilogue adds a multiple of, read as [j][i]: A (symmetric) or X^T
+  Planes out;    // written as [j][i] (A, B: symmetric; X^T)
+  Planes out2;   // kApplyB: X, written as [i][j]
+  User u;        // kApplyLast
+  Shape s;
+  int k;         // padded length of the sum
+  int ti, tj;    // tiles of i and of j
+};
+
+using lds_ptr = __attribute__((address_space(3))) void*;
+using global_ptr = const __attribute__((address_space(1))) void*;
+
+// Row r's 16-byte piece c of a stage lies at piece c ^ ((r >> 1) & 3): the 8
+// lanes that LDS serves at a time then read 8 different bank groups.
+__device__ __forceinline__ int piece(int r, int c) { return r * kDepth + ((c ^ (r >> 1)) & 3) * 8; }
+
+// A tile of kTile x kTile by four waves, a quarter each, in blocks of 32 x 32.
+// Two stages of kDepth in LDS, one being filled from memory while the other is
+// multiplied.
+template <class T, int kTile, int kStep>
+__global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
+  constexpr int kPlanes = 2, kBlocks = kTile / 64;
+  constexpr int kStage = 2 * kPlanes * kTile * kDepth;  // halves
+  __shared__ __align__(16) _Float16 lds[2 * kStage];
+  constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // neighbouring tiles on one XCD (blocks go round the 8 in turn), for its L2
+  const int total = gridDim.x, q8 = total / 8, r8 = total % 8, xcd = blockIdx.x % 8;
+  const int id = xcd * q8 + min(xcd, r8) + blockIdx.x / 8;
+  int bi, bj;
+  if constexpr (kSym) {
+    bi = (int)((__builtin_sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
+    while ((bi + 1) * (bi + 2) / 2 <= id) ++bi;
+    while (bi * (bi + 1) / 2 > id) --bi;
+    bj = id - bi * (bi + 1) / 2;
+  } else {
+    // columns of 8 tiles
+    const int band = id / (8 * a.tj), in = id - band * 8 * a.tj;
+    const int high = min(8, a.ti - band * 8);
+    bj = in / high;
+    bi = band * 8 + in - bj * high;
+  }
+  const _Float16* P = a.P.p + blockIdx.z * a.P.batch + (int64_t)bi * kTile * a.P.ld;
+  const _Float16* Q = a.Q.p + blockIdx.z * a.Q.batch + (int64_t)bj * kTile * a.Q.ld;
+
+  // 16 rows of a plane a load: lane l fetches piece (l & 3) ^ ... of row l / 4
+  const auto fill = [&](int stage, int k0) {
+    constexpr int kLoads = 2 * kPlanes * kTile / 16;
+#pragma unroll
+    for (int q = 0; q < kLoads / 4; ++q) {
+      const int seg = q * 4 + wave;
+      const int plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
+      const Planes& o = plane < kPlanes ? a.P : a.Q;
+      const _Float16* from = (plane < kPlanes ? P : Q) + (plane % kPlanes) * o.plane;
+      from += (int64_t)(rows + lane / 4) * o.ld + k0 + (((lane & 3) ^ (lane >> 3)) & 3) * 8;
+      _Float16* to = lds + stage * kStage + plane * kTile * kDepth + rows * kDepth;
+      __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)to, 16, 0, 0);
+    }
+  };
+
+  float16v acc[kBlocks][kBlocks];
+#pragma unroll
+  for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
+
+  const int wi = (wave >> 1) * (kTile / 2), wj = (wave & 1) * (kTile / 2);
+  const int stages = a.k / kDepth;
+  fill(0, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int t = 0; t < stages; ++t) {
+    if (t + 1 < stages) fill((t + 1) & 1, (t + 1) * kDepth);
+    const _Float16* st = lds + (t & 1) * kStage;
+#pragma unroll
+    for (int h = 0; h < kDepth / 16; ++h) {
+      half8 p[kBlocks][kPlanes], q[kBlocks][kPlanes];
+      const int c = h * 2 + lane / 32;
+#pragma unroll
+      for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+        for (int e = 0; e < kPlanes; ++e) {
+          p[x][e] = *reinterpret_cast<const half8*>(st + e * kTile * kDepth + piece(wi + x * 32 + (lane & 31), c));
+          q[x][e] = *reinterpret_cast<const half8*>(st + (kPlanes + e) * kTile * kDepth +
+                                                    piece(wj + x * 32 + (lane & 31), c));
+        }
+#pragma unroll
+      for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+        for (int y = 0; y < kBlocks; ++y) {
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][0], acc[x][y], 0, 0, 0);
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][1], acc[x][y], 0, 0, 0);
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][1], q[y][0], acc[x][y], 0, 0, 0);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+
+  // Epilogue. A lane holds column j = lane % 32 of each block, rows i in fours.
+  const _Float16* add = kStep == kSquareX ? nullptr : a.add.p + blockIdx.z * a.add.batch;
+  _Float16* out = kStep == kApplyLast ? nullptr : a.out.p + blockIdx.z * a.out.batch;
+#pragma unroll
+  for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int i = bi * kTile + wi + x * 32 + f * 8 + (lane >> 5) * 4;
+        const int j = bj * kTile + wj + y * 32 + (lane & 31);
+        float v[4];
+        if constexpr (kStep == kSquareX) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[x][y][f * 4 + e] * 0x1p-15f;
+        } else {
+          const int64_t at = (int64_t)j * a.add.ld + i;
+          const half4 hi = *reinterpret_cast<const half4*>(add + at);
+          const half4 lo = *reinterpret_cast<const half4*>(add + a.add.plane + at);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float old = (float)hi[e] + (float)lo[e];
+            v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, acc[x][y][f * 4 + e], kB * 0.5f * old)
+                                     : __builtin_fmaf(0x1p-14f, acc[x][y][f * 4 + e], kA * old);
+          }
+        }
+        if constexpr (kStep == kApplyLast) {
+          T* to = static_cast<T*>(a.u.out) + blockIdx.z * a.u.o_batch;
+          if (j < a.s.n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (i + e < a.s.m)
+                to[a.s.turned ? j * a.u.o_row + i + e : (i + e) * a.u.o_row + j] = (T)(v[e] * 0x1p-15f);
+          }
+        } else {
+          half4 hi, lo;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            _Float16 h, l;
+            split(v[e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+          }
+          const int64_t at = (int64_t)j * a.out.ld + i;
+          *reinterpret_cast<half4*>(out + at) = hi;
+          *reinterpret_cast<half4*>(out + a.out.plane + at) = lo;
+          if (kStep == kApplyB || (kSym && bi != bj)) {
+            const Planes& o = kSym ? a.out : a.out2;
+            _Float16* to = o.p + blockIdx.z * o.batch;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int64_t to_at = (int64_t)(i + e) * o.ld + j;
+              to[to_at] = hi[e];
+              to[o.plane + to_at] = lo[e];
+            }
+          }
+        }
+      }
+}
+
+struct Layout {
+  Shape s;
+  int tile;
+  int64_t xs, as;  // elements of a plane of X and of A
+  int64_t sums, bytes;  // offset of the sums of squares; all
+};
+
+// Tiles of 128 unless they are fewer than the device's units.
+Layout layout(int64_t batch, int64_t rows, int64_t cols) {
+  Layout l;
+  l.s.turned = rows > cols;
+  l.s.m = (int)std::min(rows, cols);
+  l.s.n = (int)std::max(rows, cols);
+  const auto up = [](int64_t v, int64_t t) { return (v + t - 1) / t * t; };
+  const int64_t t128 = up(l.s.m, 128) / 128;
+  l.tile = batch * t128 * (t128 + 1) / 2 >= 256 ? 128 : 64;
+  l.s.mp = (int)up(l.s.m, l.tile);
+  l.s.np = (int)up(l.s.n, l.tile);
+  l.xs = (int64_t)l.s.mp * l.s.np;
+  l.as = (int64_t)l.s.mp * l.s.mp;
+  // X, two of X^T, A and B, two planes each
+  l.sums = batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16);
+  l.sums = up(l.sums, 256);
+  l.bytes = l.sums + batch * kNormBlocks * (int64_t)sizeof(double);
+  return l;
+}
+
+template <class T, int kTile, int kStep>
+hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
+  constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
+  const unsigned tiles = kSym ? (unsigned)(a.ti * (a.ti + 1) / 2) : (unsigned)(a.ti * a.tj);
+  hipLaunchKernelGGL((k_orth_product<T, kTile, kStep>), dim3(tiles, 1, (unsigned)batch), dim3(kThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+template <class T, int kTile>
+hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, char* work, hipStream_t st, Planes X,
+                   Planes XT0, Planes XT1, Planes A, Planes B) {
+  Planes now = XT0, next = XT1;
+  for (int k = 0; k < steps; ++k) {
+    const bool last = k + 1 == steps;
+    ProdArgs a{};
+    a.s = l.s;
+    a.u = u;
+    a.ti = a.tj = l.s.mp / kTile;
+    a.P = a.Q = X;
+    a.out = A;
+    a.k = l.s.np;
+    hipError_t e = product<float, kTile, kSquareX>(a, batch, st);
+    if (e != hipSuccess) return e;
+    a.P = a.Q = a.add = A;
+    a.out = B;
+    a.k = l.s.mp;
+    if ((e = product<float, kTile, kSquareA>(a, batch, st)) != hipSuccess) return e;
+    a.P = B;
+    a.Q = a.add = now;
+    a.out = next;
+    a.out2 = X;
+    a.tj = l.s.np / kTile;
+    e = last ? product<T, kTile, kApplyLast>(a, batch, st) : product<float, kTile, kApplyB>(a, batch, st);
+    if (e != hipSuccess) return e;
+    std::swap(now, next);
+  }
+  return hipSuccess;
+}
+
+template <class T>
+hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t rows, int64_t cols, int steps,
+                         float eps, char* work, hipStream_t st) {
+  _Float16* at = reinterpret_cast<_Float16*>(work);
+  const auto planes = [&](int64_t elems, int ld) {
+    Planes p;
+    p.p = at;
+    p.plane = elems;
+    p.batch = 2 * elems;
+    p.ld = ld;
+    at += batch * 2 * elems;
+    return p;
+  };
+  const Planes X = planes(l.xs, l.s.np), XT0 = planes(l.xs, l.s.mp), XT1 = planes(l.xs, l.s.mp),
+               A = planes(l.as, l.s.mp), B = planes(l.as, l.s.mp);
+  double* sums = reinterpret_cast<double*>(work + l.sums);
+  const int nsums = (int)std::min<int64_t>(rows, kNormBlocks);
+  hipLaunchKernelGGL((k_orth_norm<T>), dim3(nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int pr = l.s.turned ? l.s.np : l.s.mp, pc = l.s.turned ? l.s.mp : l.s.np;  // G's sides, padded
+  hipLaunchKernelGGL((k_orth_begin<T>), dim3(pc / 64, pr / 64, (unsigned)batch), dim3(kThreads), 0, st, u, l.s, sums,
+                     nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0, (int)rows, (int)cols);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  return l.tile == 128 ? iterate<T, 128>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
+                       : iterate<T, 64>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
+}
+
+int check_sizes(int64_t batch, int64_t rows, int64_t cols) {
+  if (batch < 0 || batch > 65535) return op_error(MLKV_EINVAL, "batch must be in [0, 65535]");
+  if (rows < 1 || rows > MLKV_ORTH_MAX_DIM || cols < 1 || cols > MLKV_ORTH_MAX_DIM)
+    return op_error(MLKV_EINVAL, "rows and cols must be in [1, 32768]");
+  return MLKV_OK;
+}
+
+}  // namespace
+}  // namespace mlkv
+
+using namespace mlkv;
+
+extern "C" {
+
+int64_t mlkv_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols) {
+  const int rc = check_sizes(batch, rows, cols);
+  return rc ? rc : layout(batch, rows, cols).bytes;
+}
+
+int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows,
+                       int64_t cols, int32_t steps, float eps, int dtype, void* d_out, int64_t out_batch_stride,
+                       int64_t out_row_stride, void* d_work, int64_t work_bytes, void* hip_stream) {
+  const int rc = check_sizes(batch, rows, cols);
+  if (rc) return rc;
+  const int size = dtype_size(dtype);
+  if (size == 0) return op_error(MLKV_EINVAL, "unknown dtype");
+  if (steps < 1 || steps > 64) return op_error(MLKV_EINVAL, "steps must be in [1, 64]");
+  if (!(eps > 0.0f) || std::isinf(eps)) return op_error(MLKV_EINVAL, "eps must be finite and > 0");
+  if (batch == 0) return MLKV_OK;
+  if (d_g == nullptr || d_out == nullptr) return op_error(MLKV_EINVAL, "g or out is NULL");
+  if (!all_aligned(size, size, {d_g, d_out}, {}))
+    return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
+  const int64_t span = (rows - 1) * out_row_stride + cols;
+  if (!stride_ok(row_stride, rows, cols, true) || !stride_ok(out_row_stride, rows, cols, false))
+    return op_error(MLKV_EINVAL, "row strides must be >= cols (or 0 in g)");
+  if (batch > 1 && (batch_stride < 0 || batch_stride > (int64_t(1) << 44) || !stride_ok(out_batch_stride, batch, span, false)))
+    return op_error(MLKV_EINVAL, "batch strides must not make matrices overlap");
+  if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))
+    return op_error(MLKV_EINVAL, "out may be g only with the same strides");
+  const Layout l = layout(batch, rows, cols);
+  if (d_work == nullptr || work_bytes < l.bytes)
+    return op_error(MLKV_EINVAL, "work is smaller than mlkv_orthogonalize_workspace");
+  if (!all_aligned(256, 1, {d_work}, {})) return op_error(MLKV_EINVAL, "work must be at a multiple of 256 bytes");
+  User u;
+  u.g = d_g;
+  u.out = d_out;
+  u.g_batch = batch_stride;
+  u.g_row = row_stride;
+  u.o_batch = out_batch_stride;
+  u.o_row = out_row_stride;
+  const hipError_t e = dispatch_type(dtype, [&](auto t) {
+    return orthogonalize<decltype(t)>(l, u, batch, rows, cols, steps, eps, static_cast<char*>(d_work),
+                                      static_cast<hipStream_t>(hip_stream));
+  });
+  return e == hipSuccess ? MLKV_OK : op_launch_error(e, "mlkv_orthogonalize launch");
+}
+
+}  // extern "C"

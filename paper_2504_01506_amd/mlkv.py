@@ -22,6 +22,10 @@ MLKV_NUM_KERNELS = 10
 MLKV_DEDUP_HASH, MLKV_DEDUP_RADIX = 0, 1
 DEDUP_MODES = {"hash": MLKV_DEDUP_HASH, "radix": MLKV_DEDUP_RADIX}
 MLKV_NOALLOC_MAX_KEYS = 65536
+MLKV_F32, MLKV_BF16, MLKV_F16 = 0, 1, 2
+MLKV_NORM_MAX_DIM = 16384
+MLKV_LOGITS_MAX_VOCAB, MLKV_LOGITS_MAX_TOP = 16777216, 64
+MLKV_ORTH_MAX_DIM = 32768
 
 _lib = None
 
@@ -72,6 +76,14 @@ def load() -> ctypes.CDLL:
         "mlkv_profile_enable": (INT, [P, INT]),
         "mlkv_profile_read": (INT, [P, P, P]),
         "mlkv_kernel_name": (ctypes.c_char_p, [INT]),
+        "mlkv_layer_norm": (INT, [P, I64, P, P, I64, I32, F32, INT, INT, P, I64, P]),
+        "mlkv_layer_norm_grad_workspace": (I64, [I64, I32]),
+        "mlkv_layer_norm_grad": (INT, [P, I64, P, P, I64, I64, I32, F32, INT, INT, P, I64, P, P, P, I64, P]),
+        "mlkv_log_probs_workspace": (I64, [I64, I64, I32, INT]),
+        "mlkv_log_probs": (INT, [P, I64, P, I64, I64, I32, INT, P, P, P, P, P, P, I64, P]),
+        "mlkv_log_probs_grad": (INT, [P, I64, P, P, P, P, P, I64, I64, INT, P, I64, P]),
+        "mlkv_orthogonalize_workspace": (I64, [I64, I64, I64]),
+        "mlkv_orthogonalize": (INT, [P, I64, I64, I64, I64, I64, I32, F32, INT, P, I64, I64, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -257,6 +269,54 @@ def mlkv_profile_read(t: int):
 def mlkv_kernel_name(kernel: int) -> str:
     r = load().mlkv_kernel_name(kernel)
     return r.decode() if r else None
+
+
+# the dense operators of a step (ops.py has them on tensors)
+def mlkv_layer_norm(x, x_stride: int, weight, bias, n: int, dim: int, eps: float, dtype: int, weight_dtype: int, out,
+                    out_stride: int, stream=None) -> int:
+    return load().mlkv_layer_norm(_ptr(x), x_stride, _ptr(weight), _ptr(bias), n, dim, eps, dtype, weight_dtype,
+                                  _ptr(out), out_stride, _stream(stream))
+
+
+def mlkv_layer_norm_grad_workspace(n: int, dim: int) -> int:
+    return load().mlkv_layer_norm_grad_workspace(n, dim)
+
+
+def mlkv_layer_norm_grad(x, x_stride: int, weight, grad, grad_stride: int, n: int, dim: int, eps: float, dtype: int,
+                         weight_dtype: int, x_grad, x_grad_stride: int, weight_grad, bias_grad, work, work_bytes: int,
+                         stream=None) -> int:
+    return load().mlkv_layer_norm_grad(_ptr(x), x_stride, _ptr(weight), _ptr(grad), grad_stride, n, dim, eps, dtype,
+                                       weight_dtype, _ptr(x_grad), x_grad_stride, _ptr(weight_grad), _ptr(bias_grad),
+                                       _ptr(work), work_bytes, _stream(stream))
+
+
+def mlkv_log_probs_workspace(n: int, vocab: int, top: int, dtype: int) -> int:
+    return load().mlkv_log_probs_workspace(n, vocab, top, dtype)
+
+
+def mlkv_log_probs(logits, stride: int, tokens, n: int, vocab: int, top: int, dtype: int, logp, entropy, stats,
+                   top_ids, top_logp, work, work_bytes: int, stream=None) -> int:
+    return load().mlkv_log_probs(_ptr(logits), stride, _ptr(tokens), n, vocab, top, dtype, _ptr(logp), _ptr(entropy),
+                                 _ptr(stats), _ptr(top_ids), _ptr(top_logp), _ptr(work), work_bytes, _stream(stream))
+
+
+def mlkv_log_probs_grad(logits, stride: int, tokens, stats, entropy, logp_grad, entropy_grad, n: int, vocab: int,
+                        dtype: int, logits_grad, grad_stride: int, stream=None) -> int:
+    return load().mlkv_log_probs_grad(_ptr(logits), stride, _ptr(tokens), _ptr(stats), _ptr(entropy), _ptr(logp_grad),
+                                      _ptr(entropy_grad), n, vocab, dtype, _ptr(logits_grad), grad_stride,
+                                      _stream(stream))
+
+
+def mlkv_orthogonalize_workspace(batch: int, rows: int, cols: int) -> int:
+    return load().mlkv_orthogonalize_workspace(batch, rows, cols)
+
+
+def mlkv_orthogonalize(g, batch_stride: int, row_stride: int, batch: int, rows: int, cols: int, steps: int, eps: float,
+                       dtype: int, out, out_batch_stride: int, out_row_stride: int, work, work_bytes: int,
+                       stream=None) -> int:
+    return load().mlkv_orthogonalize(_ptr(g), batch_stride, row_stride, batch, rows, cols, steps, eps, dtype,
+                                     _ptr(out), out_batch_stride, out_row_stride, _ptr(work), work_bytes,
+                                     _stream(stream))
 
 
 # ---- a small object wrapper over the same calls -----------------------------

@@ -1,0 +1,263 @@
+"""The dense operators of a training step around a table, on torch tensors.
+
+What a step computes between the get of its rows and the put_grad of their
+gradients, as far as it is row-wise (layer_norm, log_probs and their
+gradients), and the update of a dense weight that no table holds
+(orthogonalize). Each is one call of the library (include/mlkv.h says what it
+computes): tensors are checked here and passed as device pointers, outputs and
+workspaces that are not given are allocated by torch, and the work is queued on
+`stream` (the current stream of the tensors' device unless given) without
+waiting for it. There is no fallback: without the built library, or on tensors
+that are not on a GPU, a call raises.
+
+As with any torch call on a side stream, a tensor that is given and was made on
+another stream than `stream` must be ready there, and kept until the work is
+done; what a call allocates belongs to `stream`.
+"""
+from __future__ import annotations
+
+import contextlib
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import mlkv
+
+_TYPES = {torch.float32: mlkv.MLKV_F32, torch.bfloat16: mlkv.MLKV_BF16, torch.float16: mlkv.MLKV_F16}
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=None, dense=False):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{what} must be a tensor")
+    if t.device != like.device:
+        raise ValueError(f"{what} is on {t.device}, not on {like.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+
+
+def _on_gpu(t: torch.Tensor, what: str):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{what} must be a tensor on a GPU")
+    if t.is_conj() or t.is_neg():
+        raise ValueError(f"{what} must be resolved first")
+
+
+def _rows(t: torch.Tensor, what: str) -> tuple[int, int, int]:
+    """(rows, elements a row, elements from row to row) of a tensor whose last
+    dimension is the row and whose others follow one another evenly."""
+    if t.dim() == 0:
+        raise ValueError(f"{what} must have at least one dimension")
+    width = t.shape[-1]
+    if width == 0:
+        raise ValueError(f"{what} has rows of no elements")
+    n = t.numel() // width
+    if t.dim() == 1 or n <= 1:
+        if t.stride(-1) != 1 and width > 1:
+            raise ValueError(f"{what}: the elements of a row must lie next to each other")
+        return n, width, width
+    if n == 0:
+        return 0, width, width
+    if t.stride(-1) != 1 and width > 1:
+        raise ValueError(f"{what}: the elements of a row must lie next to each other")
+    stride = None
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride, reach = step, step * size
+        elif step == reach:
+            reach *= size
+        else:
+            raise ValueError(f"{what}: the rows must be evenly spaced")
+    return n, width, stride
+
+
+def _out(t: Optional[torch.Tensor], what: str, like: torch.Tensor) -> torch.Tensor:
+    if t is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    _check(t, what, like, like.dtype, like.shape)
+    return t
+
+
+@contextlib.contextmanager
+def _queue(t: torch.Tensor, stream):
+    """Makes the tensor's device current, and `stream` its current stream; yields the stream's handle."""
+    with torch.cuda.device(t.device):
+        if stream is None:
+            yield torch.cuda.current_stream().cuda_stream
+            return
+        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        if s.device != t.device:
+            raise ValueError(f"the stream is of {s.device}, the tensors are on {t.device}")
+        with torch.cuda.stream(s):
+            yield s.cuda_stream
+
+
+def _bytes(n: int) -> int:
+    if n < 0:
+        raise mlkv.MlkvError(n, mlkv.last_error())
+    return n
+
+
+def _params(x: torch.Tensor, dim: int, **params) -> int:
+    """Checks a weight and a bias (fp32 or of x's type, the same for both); their type's code."""
+    kind = None
+    for what, p in params.items():
+        if p is None:
+            continue
+        _check(p, what, x, shape=(dim,), dense=True)
+        if p.dtype not in (torch.float32, x.dtype):
+            raise ValueError(f"{what} must be float32 or {x.dtype}, not {p.dtype}")
+        if kind not in (None, p.dtype):
+            raise ValueError("weight and bias must be of one type")
+        kind = p.dtype
+    return _TYPES[kind or x.dtype]
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Layer norm over the last dimension of x ([..., dim], fp32, bf16 or fp16);
+    weight and bias ([dim], fp32 or of x's type) may be None. `out` may be x."""
+    _on_gpu(x, "x")
+    kind = _dtype(x, "x")
+    n, dim, step = _rows(x, "x")
+    wkind = _params(x, dim, weight=weight, bias=bias)
+    with _queue(x, stream) as st:
+        out = _out(out, "out", x)
+        ostep = _rows(out, "out")[2]
+        mlkv._check(mlkv.mlkv_layer_norm(x, step, weight, bias, n, dim, eps, kind, wkind, out, ostep, st))
+    return out
+
+
+def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch.Tensor, eps: float = 1e-5,
+                    out: Optional[torch.Tensor] = None, stream=None):
+    """(x_grad, weight_grad, bias_grad) of layer_norm(x, weight, bias, eps) for
+    the gradient `grad` of its output. x_grad is of x's type (rows for a
+    table's put_grad where that is fp32) and goes to `out` if given (which may
+    be grad or x); the other two are of weight's type, or x's without a weight."""
+    _on_gpu(x, "x")
+    kind = _dtype(x, "x")
+    n, dim, step = _rows(x, "x")
+    wkind = _params(x, dim, weight=weight)
+    _check(grad, "grad", x, x.dtype, x.shape)
+    gstep = _rows(grad, "grad")[2]
+    with _queue(x, stream) as st:
+        out = _out(out, "out", x)
+        ostep = _rows(out, "out")[2]
+        wtype = x.dtype if weight is None else weight.dtype
+        dw = torch.empty(dim, dtype=wtype, device=x.device)
+        db = torch.empty(dim, dtype=wtype, device=x.device)
+        nbytes = _bytes(mlkv.mlkv_layer_norm_grad_workspace(n, dim))
+        work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+        mlkv._check(mlkv.mlkv_layer_norm_grad(x, step, weight, grad, gstep, n, dim, eps, kind, wkind, out, ostep, dw,
+                                              db, work, nbytes, st))
+    return out, dw, db
+
+
+class LogProbs(NamedTuple):
+    logp: torch.Tensor                   # fp32, the tokens' shape
+    entropy: torch.Tensor                # fp32
+    stats: torch.Tensor                  # fp32 [..., 2]: largest logit, log of the sum of exp(logit - largest)
+    top_ids: Optional[torch.Tensor]      # int64 [..., top], largest first, equal ones lowest index first
+    top_logp: Optional[torch.Tensor]     # fp32 [..., top]
+
+
+def log_probs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, stream=None) -> LogProbs:
+    """Log probability of tokens[...] (int64; < 0: none, gives 0) under
+    logits[..., vocab], the distribution's entropy, and the `top` (<= 64) most
+    likely alternatives. `stats` and `entropy` are what log_probs_grad takes."""
+    _on_gpu(logits, "logits")
+    kind = _dtype(logits, "logits")
+    n, vocab, step = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    _check(tokens, "tokens", logits, torch.int64, lead, dense=True)
+    top = int(top)
+    with _queue(logits, stream) as st:
+        nbytes = _bytes(mlkv.mlkv_log_probs_workspace(n, vocab, top, kind))
+
+        def new(*tail, dtype=torch.float32):
+            return torch.empty((*lead, *tail), dtype=dtype, device=logits.device)
+
+        r = LogProbs(new(), new(), new(2), new(top, dtype=torch.int64) if top else None, new(top) if top else None)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+        mlkv._check(mlkv.mlkv_log_probs(logits, step, tokens, n, vocab, top, kind, r.logp, r.entropy, r.stats,
+                                        r.top_ids, r.top_logp, work, nbytes, st))
+    return r
+
+
+def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: torch.Tensor,
+                   entropy: Optional[torch.Tensor], logp_grad: Optional[torch.Tensor],
+                   entropy_grad: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """Gradient in the logits, for the gradients logp_grad and entropy_grad
+    (fp32, either may be None) of log_probs' first two outputs; `out` may be logits."""
+    _on_gpu(logits, "logits")
+    kind = _dtype(logits, "logits")
+    n, vocab, step = _rows(logits, "logits")
+    lead = logits.shape[:-1]
+    if logp_grad is not None:
+        _check(logp_grad, "logp_grad", logits, torch.float32, lead, dense=True)
+        if tokens is None:
+            raise ValueError("logp_grad needs tokens")
+    if tokens is not None:
+        _check(tokens, "tokens", logits, torch.int64, lead, dense=True)
+    _check(stats, "stats", logits, torch.float32, (*lead, 2), dense=True)
+    if entropy_grad is not None:
+        _check(entropy_grad, "entropy_grad", logits, torch.float32, lead, dense=True)
+        if entropy is None:
+            raise ValueError("entropy_grad needs entropy")
+    if entropy is not None:
+        _check(entropy, "entropy", logits, torch.float32, lead, dense=True)
+    with _queue(logits, stream) as st:
+        out = _out(out, "out", logits)
+        ostep = _rows(out, "out")[2]
+        mlkv._check(mlkv.mlkv_log_probs_grad(logits, step, tokens, stats, entropy, logp_grad, entropy_grad, n, vocab,
+                                             kind, out, ostep, st))
+    return out
+
+
+def _matrices(t: torch.Tensor, what: str) -> tuple[int, int]:
+    """(elements from matrix to matrix, from row to row) of [rows, cols] or [batch, rows, cols]."""
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: the elements of a row must lie next to each other")
+    row = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+    if t.dim() == 2 or t.shape[0] <= 1:
+        return t.shape[-2] * t.shape[-1], row
+    return t.stride(0), row
+
+
+def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """The update g ([rows, cols], or [batch, rows, cols] for a stack of them;
+    fp32, bf16 or fp16) made nearly orthogonal by `steps` Newton-Schulz steps:
+    the same singular vectors, singular values near 1. `out` may be g. A
+    transposed view is taken as it lies: its transpose is worked on."""
+    _on_gpu(g, "g")
+    kind = _dtype(g, "g")
+    if g.dim() not in (2, 3):
+        raise ValueError("g must have 2 or 3 dimensions")
+    if g.shape[-1] == 0 or g.shape[-2] == 0:
+        raise ValueError("g has matrices of no elements")
+    if g.stride(-1) != 1 and g.stride(-2) == 1 and g.shape[-1] > 1:
+        return orthogonalize(g.mT, steps, eps, None if out is None else out.mT, stream).mT
+    batch = g.shape[0] if g.dim() == 3 else 1
+    rows, cols = g.shape[-2:]
+    gb, gr = _matrices(g, "g")
+    with _queue(g, stream) as st:
+        out = _out(out, "out", g)
+        ob, orow = _matrices(out, "out")
+        nbytes = _bytes(mlkv.mlkv_orthogonalize_workspace(batch, rows, cols))
+        work = torch.empty(nbytes, dtype=torch.uint8, device=g.device)
+        mlkv._check(mlkv.mlkv_orthogonalize(g, gb, gr, batch, rows, cols, int(steps), eps, kind, out, ob, orow, work,
+                                            nbytes, st))
+    return out

@@ -1,0 +1,238 @@
+"""Orthogonalised updates against the iteration in 64 bits.
+
+Tolerance: a step's operands carry 2^-22 each and its sums the rounding of
+fp32, so a step adds an error of at most 2^-18 ||X|| to X (three products of
+matrices of norms up to 1.21, 1.45 and 2.81, with sums of length m or n whose
+roundings add like their square root), and 2^-40 an element where that is more. The steps behind it stretch an error by
+their largest slope over the singular values there. The bound sums these over
+the steps; 16-bit outputs add half a step of theirs."""
+import math
+
+import pytest
+import torch
+
+from paper_2504_01506_amd import mlkv
+
+A, B, C = 3.4445, -4.7750, 2.0315
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def quintic(s):
+    return A * s + B * s ** 3 + C * s ** 5
+
+
+def slope(s):
+    return (A + 3 * B * s ** 2 + 5 * C * s ** 4).abs()
+
+
+def reference(g, steps, eps):
+    """(the result, the bound on the error's norm) of one matrix in 64 bits."""
+    x = g.double()
+    turned = x.shape[0] > x.shape[1]
+    if turned:
+        x = x.t().contiguous()
+    x = x / (x.norm() + eps)
+    sizes, slopes = [], []
+    for _ in range(steps):
+        # between the smallest and the largest singular value, and a little beyond
+        hi = torch.linalg.matrix_norm(x, 2)
+        slopes.append(slope(torch.linspace(0, float(hi) * 1.001, 2001, dtype=torch.float64)).max())
+        q = x @ x.t().contiguous()
+        x = A * x + B * (q @ x) + C * (q @ (q @ x))
+        sizes.append(x.norm())
+    far, bound = 1.0, 0.0
+    for k in reversed(range(steps)):
+        bound += far * (2.0 ** -18 * float(sizes[k]) + 2.0 ** -40 * math.sqrt(x.numel()))
+        far *= float(slopes[k])
+    return (x.t() if turned else x), bound
+
+
+def check(g, steps=5, eps=1e-7, out=None, steep=False):
+    from paper_2504_01506_amd import ops
+    keep = g.clone()
+    got = ops.orthogonalize(g, steps, eps, out=out)
+    assert got.shape == g.shape and got.dtype == g.dtype
+    for k, m in enumerate(keep if g.dim() == 3 else keep[None]):
+        want, bound = reference(m, steps, eps)
+        have = (got[k] if g.dim() == 3 else got).double()
+        off = (have - want).norm().item()
+        bound += (torch.finfo(g.dtype).eps / 2 * want.norm() +
+                  math.sqrt(want.numel()) * torch.finfo(g.dtype).smallest_normal).item()
+        assert off <= bound, (off, bound)
+        # as exact as a product in fp32 of 16 roundings would be, whatever the bound allows
+        if g.dtype == torch.float32 and not steep:
+            assert off <= 2e-5 * max(want.norm().item(), 1e-30)
+    return got
+
+
+@pytest.fixture
+def gen():
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    return g
+
+
+def update(gen, *shape, kind=torch.float32, scale=0.01):
+    return (scale * torch.randn(shape, generator=gen, device="cuda")).to(kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (9, 1), (2, 2), (3, 64), (63, 65), (64, 64), (65, 63), (64, 250),
+                                       (250, 64), (127, 129), (128, 128), (200, 1000), (1000, 200), (513, 511)])
+def test_shapes(gen, rows, cols, kind):
+    check(update(gen, rows, cols, kind=kind))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,rows,cols", [(1, 40, 50), (7, 33, 90), (16, 64, 250), (3, 300, 130), (130, 60, 20),
+                                             (40, 384, 384)])
+def test_stacks(gen, batch, rows, cols):
+    check(update(gen, batch, rows, cols))
+    check(update(gen, batch, rows, cols, kind=torch.bfloat16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(3000, 2900), (2048, 4096)])
+def test_large(gen, rows, cols):
+    check(update(gen, rows, cols))
+    check(update(gen, rows, cols, kind=torch.float16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+def test_steps_and_scales(gen, steps):
+    for scale in (1e-6, 1.0, 1e4):
+        check(update(gen, 70, 200, scale=scale), steps)
+    check(update(gen, 70, 200), steps, eps=0.5)      # an eps as large as the norm
+    check(update(gen, 70, 200, scale=1e-20), steps, steep=True)  # a norm far below eps
+    check(update(gen, 70, 200, scale=1e25), steps)   # squares beyond fp32
+
+
+@pytest.mark.gpu
+def test_known_singular_values(gen):
+    # U diag(s) V': the steps act on the singular values alone
+    u = torch.linalg.qr(torch.randn((90, 90), generator=gen, device="cuda").double())[0]
+    v = torch.linalg.qr(torch.randn((300, 90), generator=gen, device="cuda").double())[0]
+    s = torch.logspace(0, -2, 90, device="cuda").double()
+    from paper_2504_01506_amd import ops
+    got = ops.orthogonalize((u * s @ v.t().contiguous()).float()).double()
+    t = s / (s.norm() + 1e-7)
+    for _ in range(5):
+        t = quintic(t)
+    want = u * t @ v.t().contiguous()
+    # the input's own rounding, 2^-24 of its norm, is stretched by at most A^5 = 485
+    assert (got - want).norm() <= (485 * 2.0 ** -24 * 2 + 2e-5) * want.norm()
+    assert t.min() > 0.6 and t.max() < 1.21
+
+
+@pytest.mark.gpu
+def test_low_rank_zeros_and_values_out_of_range(gen):
+    from paper_2504_01506_amd import ops
+    # the rounding of X to pairs, 2^-23 of its norm, lies all but for a part of 1/80 in directions of singular value 0,
+    # which five steps stretch A^5 = 485 times: 485 * 2^-23 = 5.8e-5 alone, so that only the bound is asked for here
+    check(torch.randn((80, 1), generator=gen, device="cuda") @ torch.randn((1, 100), generator=gen, device="cuda"),
+          steep=True)
+    stack = update(gen, 5, 100, 70)
+    stack[1] = 0
+    stack[2, 3, 4] = float("nan")
+    stack[3, 0, 0] = float("inf")
+    stack[4, 50:] = 0
+    out = ops.orthogonalize(stack)
+    assert (out[1] == 0).all() and torch.isnan(out[2]).all() and torch.isnan(out[3]).all()
+    check(stack[[0, 4]])
+    assert ops.orthogonalize(stack[:0]).shape == (0, 100, 70)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_strides_transposes_and_in_place(gen, kind):
+    from paper_2504_01506_amd import ops
+    buf = update(gen, 4, 90, 210, kind=kind)
+    g = buf[1:3, 5:75, 3:203]
+    want = check(g)
+    t = check(g.mT)
+    assert t.stride(-1) != 1
+    assert torch.equal(t, ops.orthogonalize(g).mT)
+    assert torch.equal(ops.orthogonalize(g.mT.contiguous()), want.mT)   # the same products either way
+    hold = torch.full((3, 80, 220), 8.0, dtype=kind, device="cuda")
+    out = hold[:2, :70, 10:210]
+    assert ops.orthogonalize(g, out=out) is out and torch.equal(out, want)
+    assert (hold[2] == 8).all() and (hold[:, 70:] == 8).all() and (hold[:, :, :10] == 8).all()
+    assert (hold[:, :, 210:] == 8).all()
+    same = g[0].expand(3, 70, 200)
+    assert torch.equal(ops.orthogonalize(same), want[:1].expand(3, 70, 200))
+    before = buf.clone()
+    assert torch.equal(ops.orthogonalize(g, out=g), want)
+    before[1:3, 5:75, 3:203] = want
+    assert torch.equal(buf, before)
+
+
+@pytest.mark.gpu
+def test_streams_and_graph_replays(gen):
+    from paper_2504_01506_amd import ops
+    g, g2 = update(gen, 300, 500), update(gen, 6, 64, 90, kind=torch.bfloat16)
+    want, want2 = ops.orthogonalize(g), ops.orthogonalize(g2)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        got, got2 = ops.orthogonalize(g, stream=a), ops.orthogonalize(g2, stream=b.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(got2, want2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, got2 = ops.orthogonalize(g), ops.orthogonalize(g2)
+    for k in range(3):
+        g.add_(0.01 * k), g2.mul_(1 + k)
+        graph.replay()
+        assert torch.equal(got, ops.orthogonalize(g)) and torch.equal(got2, ops.orthogonalize(g2))
+        torch.cuda.synchronize()
+
+
+# ---- refusals (no GPU needed: nothing is launched) ----
+def call(**change):
+    a = dict(g=4096, gb=6400, gr=100, batch=2, rows=64, cols=100, steps=5, eps=1e-7, dtype=mlkv.MLKV_F32, out=2 ** 20,
+             ob=6400, orow=100, work=2 ** 24, bytes=2 ** 24)
+    a.update(change)
+    return mlkv.mlkv_orthogonalize(a["g"], a["gb"], a["gr"], a["batch"], a["rows"], a["cols"], a["steps"], a["eps"],
+                                   a["dtype"], a["out"], a["ob"], a["orow"], a["work"], a["bytes"], 0)
+
+
+@pytest.mark.parametrize("change,says", [
+    (dict(batch=-1), "batch"), (dict(batch=65536), "batch"), (dict(rows=0), "rows and cols"),
+    (dict(cols=32769), "rows and cols"), (dict(steps=0), "steps"), (dict(steps=65), "steps"), (dict(eps=0.0), "eps"),
+    (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(dtype=3), "dtype"), (dict(g=None), "NULL"),
+    (dict(out=None), "NULL"), (dict(gr=99), "row strides"), (dict(orow=0), "row strides"), (dict(gb=-1), "overlap"),
+    (dict(ob=6399), "overlap"), (dict(ob=0), "overlap"), (dict(out=4096, orow=101, ob=6464), "same strides"),
+    (dict(work=None), "work"), (dict(bytes=1000), "work"), (dict(work=2 ** 24 + 128), "work"),
+    (dict(g=4097), "aligned"), (dict(out=2 ** 20 + 2), "aligned")])
+def test_refusals(change, says):
+    assert call(**change) == mlkv.MLKV_EINVAL
+    assert says in mlkv.last_error()
+
+
+def test_workspace_sizes():
+    size = mlkv.mlkv_orthogonalize_workspace
+    assert size(0, 5, 5) == 0 and size(1, 64, 64) > 0
+    assert size(1, 100, 70) == size(1, 70, 100)
+    for bad in ((-1, 5, 5), (1, 0, 5), (1, 5, 32769), (65536, 1, 1)):
+        assert size(*bad) == mlkv.MLKV_EINVAL
+
+
+def test_tensors_are_checked():
+    from paper_2504_01506_amd import ops
+    with pytest.raises(ValueError, match="GPU"):
+        ops.orthogonalize(torch.zeros((3, 4)))
+
+
+@pytest.mark.gpu
+def test_tensors_are_checked_on_the_gpu():
+    from paper_2504_01506_amd import ops
+    g = torch.zeros((4, 6), device="cuda")
+    for bad in (lambda: ops.orthogonalize(g[0]), lambda: ops.orthogonalize(g[:, :0]),
+                lambda: ops.orthogonalize(g.double()), lambda: ops.orthogonalize(g[:, ::2]),
+                lambda: ops.orthogonalize(g, out=g.t()), lambda: ops.orthogonalize(g, out=g.half())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(mlkv.MlkvError, match="steps"):
+        ops.orthogonalize(g, steps=0)
