@@ -398,12 +398,6 @@ struct GradArgs {
   int vocab, chunks;
 };
 
-// V elements at any address of T.
-template <class T, int V>
-struct __attribute__((packed, aligned(sizeof(T)))) LoosePack {
-  T v[V];
-};
-
 constexpr int kGradVecs = 4;  // vectors of a thread
 
 // One logit's gradient: g its row's a, b and stats.

@@ -1,11 +1,17 @@
 // Layer norm and its gradient.
 //
 // A row belongs to a group of G lanes that holds it whole in registers, I
-// vectors of V elements a lane, so each element is read once and both passes
-// of the variance (mean, then squares about it) run on registers. Rows of up
-// to 1024 elements have a group within a wave, several groups a block; longer
-// ones have a block of waves each that exchange their sums through LDS. Both
-// kernels are bound by HBM: 8 and 16 operations an element against 4 to 12 bytes.
+// vectors of 16 bytes a lane at any alignment, so each element is read once
+// and both passes of the variance (mean, then squares about it) run on
+// registers. Rows of up to 1024 elements have a group within a wave, several
+// groups a block; longer ones have a block of waves each that exchange their
+// sums through LDS. Both kernels are bound by HBM: 8 and 16 operations an
+// element against 4 to 12 bytes.
+//
+// A row's loads are whole vectors in every lane, so that the next row's are in
+// flight while a row is worked on: the vector that would reach past the row's
+// end is moved back to end there and takes part with its last elements only,
+// and a lane without any reads that vector too.
 #include "mlkv_ops.h"
 
 #include <algorithm>
@@ -15,12 +21,9 @@ namespace mlkv {
 namespace {
 
 constexpr int kNormThreads = 256;      // of a block of groups within waves
-constexpr int kNormMaxThreads = 1024;  // of a block that holds one row
-
-// Most blocks of a gradient call that sums over rows: each leaves 2 * dim floats of sums.
-constexpr int kGradBlocksNarrow = 2048;
-constexpr int kGradBlocksWide = 512;
-inline int grad_blocks_max(int32_t dim) { return dim <= 1024 ? kGradBlocksNarrow : kGradBlocksWide; }
+// Threads of a block that holds one row: up to kNormMidThreads the row after
+// the present one is loaded ahead; more threads have too few registers for it.
+constexpr int kNormMidThreads = 512, kNormMaxThreads = 1024;
 
 struct NormArgs {
   const void* x;
@@ -40,18 +43,18 @@ struct NormArgs {
 // A row's sums over the block's waves (rows that a whole block holds).
 template <int N>
 __device__ __forceinline__ void block_sums(float (&v)[N], float* lds) {
-  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     v[k] = group_sum(v[k], 64);
-    if ((threadIdx.x & 63) == 0) lds[wave * N + k] = v[k];
+    if (lane == 0) lds[wave * N + k] = v[k];
   }
   __syncthreads();
+  const int from = lane & 15;  // (at most 16 waves)
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = 0.0f;
-  for (int w = 0; w < waves; ++w)
+  for (int k = 0; k < N; ++k) v[k] = from < waves ? lds[from * N + k] : 0.0f;
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += lds[w * N + k];
+  for (int k = 0; k < N; ++k) v[k] = group_sum(v[k], 16);
 }
 
 template <bool kBlock, int N>
@@ -64,78 +67,116 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int G, float* lds) {
   }
 }
 
-template <class T, int V, int I>
-struct Row {
-  Pack<T, V> p[I];
-  // Loads the lane's vectors; zeros where it has none.
-  __device__ __forceinline__ void load(const T* row, int l, int G, int nvec, bool live) {
+// The columns of lane l: vector i begins at column at[i], and its elements
+// from skip[i] on are the lane's own (all where kFull: a row is G * I vectors).
+// Rows shorter than a vector (kShort) are loaded by elements, a lane a row.
+template <class T, int I, bool kFull>
+struct Columns {
+  static constexpr int V = 16 / sizeof(T);
+  int at[I], skip[I];
+  __device__ __forceinline__ Columns(int l, int G, int dim) {
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      const int v = i * G + l;
-      if (live && v < nvec) {
-        p[i] = *reinterpret_cast<const Pack<T, V>*>(row + (int64_t)v * V);
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) p[i].v[j] = (T)0.0f;
-      }
+      const int c = (i * G + l) * V;
+      at[i] = kFull ? c : max(min(c, dim - V), 0);
+      skip[i] = kFull ? 0 : min(c - at[i], V);
     }
   }
+  __device__ __forceinline__ bool own(int i, int j) const { return kFull || j >= skip[i]; }
 };
 
-template <class T>
-__device__ __forceinline__ float param(const void* p, bool wide, int c) {
-  return wide ? static_cast<const float*>(p)[c] : (float)static_cast<const T*>(p)[c];
+template <class T, int I, bool kFull, bool kShort>
+__device__ __forceinline__ void load_row(Raw (&p)[I], const T* row, const Columns<T, I, kFull>& cols, int dim) {
+  if constexpr (kShort) {
+    constexpr int V = 16 / sizeof(T);
+    union {
+      Raw r;
+      T v[V];
+    } u;
+    u.r = Raw{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < V - 1; ++j)
+      if (j < dim) u.v[j] = row[j];
+    p[0] = u.r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < I; ++i) p[i] = load_raw(row + cols.at[i]);
+  }
 }
 
-// One thread's columns of weight or bias.
-template <class T, int V, int I>
-__device__ __forceinline__ void load_params(float (&w)[I * V], const void* p, bool wide, float none, int l, int G,
-                                            int nvec) {
+template <class T, int V, bool kShort>
+__device__ __forceinline__ void store_row(T* row, int c, int dim, const LoosePack<T, V>& o) {
+  if constexpr (kShort) {
+#pragma unroll
+    for (int j = 0; j < V - 1; ++j)
+      if (j < dim) row[j] = o.v[j];
+  } else {
+    *reinterpret_cast<LoosePack<T, V>*>(row + c) = o;
+  }
+}
+
+// One thread's columns of weight or bias; `none` in those that are not its own.
+template <class T, int I, bool kFull, bool kShort>
+__device__ __forceinline__ void load_params(float (&w)[I * (16 / sizeof(T))], const void* p, bool wide, float none,
+                                            const Columns<T, I, kFull>& cols, int dim) {
+  constexpr int V = 16 / sizeof(T);
 #pragma unroll
   for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int v = i * G + l;
-      w[i * V + j] = p != nullptr && v < nvec ? param<T>(p, wide, v * V + j) : none;
+      const int c = cols.at[i] + j;
+      w[i * V + j] = none;
+      if (p != nullptr && (!kShort || c < dim))
+        w[i * V + j] = wide ? static_cast<const float*>(p)[c] : (float)static_cast<const T*>(p)[c];
     }
 }
 
-template <class T, int V, int I, bool kBlock>
-__global__ __launch_bounds__(kBlock ? kNormMaxThreads : kNormThreads) void k_layer_norm(NormArgs a) {
+// kMost: threads of a block at most, 0 for rows within waves
+template <class T, int I, int kMost, bool kFull, bool kShort>
+__global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(NormArgs a) {
   __shared__ float lds1[kNormMaxThreads / 64];
   __shared__ float lds2[2 * kNormMaxThreads / 64];
-  const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1);
+  constexpr int V = 16 / sizeof(T);
+  constexpr bool kBlock = kMost != 0, kAhead = kMost != kNormMaxThreads;
+  const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1), dim = a.dim;
   const int per = kBlock ? 1 : kNormThreads / G;
-  const int nvec = a.dim / V;
-  const float inv = 1.0f / (float)a.dim;
+  const float inv = 1.0f / (float)dim;
+  const Columns<T, I, kFull> cols(l, G, dim);
+  // (kShort: a lane has a row of its own, elements from dim on are not)
+  const auto own = [&](int i, int j) { return kShort ? j < dim : cols.own(i, j); };
   float w[I * V], b[I * V];
-  load_params<T, V, I>(w, a.weight, a.wide_weight, 1.0f, l, G, nvec);
-  load_params<T, V, I>(b, a.bias, a.wide_weight, 0.0f, l, G, nvec);
-  const int sub = kBlock ? 0 : threadIdx.x / G;
-  Row<T, V, I> next;
-  int64_t r = (int64_t)blockIdx.x * per + sub;
+  load_params<T, I, kFull, kShort>(w, a.weight, a.wide_weight, 1.0f, cols, dim);
+  load_params<T, I, kFull, kShort>(b, a.bias, a.wide_weight, 0.0f, cols, dim);
+  int64_t r = (int64_t)blockIdx.x * per + (kBlock ? 0 : threadIdx.x / G);
   const int64_t step = (int64_t)gridDim.x * per;
-  next.load(static_cast<const T*>(a.x) + r * a.x_stride, l, G, nvec, r < a.n);
+  Raw next[I] = {};
+  const auto load = [&](int64_t row) {
+    if (row < a.n) load_row<T, I, kFull, kShort>(next, static_cast<const T*>(a.x) + row * a.x_stride, cols, dim);
+  };
+  if constexpr (kAhead) load(r);
   for (int64_t base = (int64_t)blockIdx.x * per; base < a.n; base += step, r += step) {
-    const Row<T, V, I> cur = next;
-    next.load(static_cast<const T*>(a.x) + (r + step) * a.x_stride, l, G, nvec, r + step < a.n);
+    if constexpr (!kAhead) load(r);
+    float x[I * V];
     float s[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[0] += (float)cur.p[i].v[j];
+      for (int j = 0; j < V; ++j) {
+        x[i * V + j] = element<T>(next[i], j);
+        s[0] += own(i, j) ? x[i * V + j] : 0.0f;
+      }
+    if constexpr (kAhead) load(r + step);
     row_sums<kBlock>(s, G, lds1);
     const float mean = s[0] * inv;
     float q[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < I; ++i)
-      if (i * G + l < nvec) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float d = (float)cur.p[i].v[j] - mean;
-          q[0] += d;
-          q[1] = __builtin_fmaf(d, d, q[1]);
-        }
+      for (int j = 0; j < V; ++j) {
+        x[i * V + j] -= mean;
+        const float d = own(i, j) ? x[i * V + j] : 0.0f;
+        q[0] += d;
+        q[1] = __builtin_fmaf(d, d, q[1]);
       }
     row_sums<kBlock>(q, G, lds2);
     // what the rounding of `mean` left over, out of the variance and the differences
@@ -146,16 +187,12 @@ __global__ __launch_bounds__(kBlock ? kNormMaxThreads : kNormThreads) void k_lay
       T* out = static_cast<T*>(a.out) + r * a.out_stride;
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        const int v = i * G + l;
-        if (v < nvec) {
-          Pack<T, V> o;
+        LoosePack<T, V> o;
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const float h = (((float)cur.p[i].v[j] - mean) - off) * rstd;
-            o.v[j] = (T)__builtin_fmaf(h, w[i * V + j], b[i * V + j]);
-          }
-          *reinterpret_cast<Pack<T, V>*>(out + (int64_t)v * V) = o;
-        }
+        for (int j = 0; j < V; ++j)
+          o.v[j] = (T)__builtin_fmaf((x[i * V + j] - off) * rstd, w[i * V + j], b[i * V + j]);
+        // (elements that are another lane's too get the same value from both)
+        if (kFull || kShort || cols.skip[i] < V) store_row<T, V, kShort>(out, cols.at[i], dim, o);
       }
     }
   }
@@ -164,49 +201,63 @@ __global__ __launch_bounds__(kBlock ? kNormMaxThreads : kNormThreads) void k_lay
 // The gradient. After the mean one exchange gives the four sums that the rest
 // needs: of d = x - mean, d^2, g and g d. Each thread keeps the sums over rows
 // of its own columns in registers; a block joins them at its end.
-template <class T, int V, int I, bool kBlock>
-__global__ __launch_bounds__(kBlock ? kNormMaxThreads : kNormThreads) void k_layer_norm_grad(NormArgs a) {
+// (whole 16-bit rows a block: four waves a SIMD, 128 registers)
+template <class T, int I, int kMost, bool kFull, bool kShort>
+__global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMost && kFull ? 4 : 1) void k_layer_norm_grad(NormArgs a) {
   __shared__ float lds1[kNormMaxThreads / 64];
-  __shared__ float lds2[4 * kNormMaxThreads / 64];
-  extern __shared__ float join[];  // [groups of the block][G * I * V] (not kBlock)
-  const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1);
+  __shared__ __align__(16) float lds2[4 * kNormMaxThreads / 64];
+  extern __shared__ __align__(16) float join[];  // [groups of the block][G * I * V] (not kBlock)
+  constexpr int V = 16 / sizeof(T);
+  constexpr bool kBlock = kMost != 0, kAhead = kMost != kNormMaxThreads;
+  const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1), dim = a.dim;
   const int per = kBlock ? 1 : kNormThreads / G;
-  const int nvec = a.dim / V;
-  const float inv = 1.0f / (float)a.dim;
+  const float inv = 1.0f / (float)dim;
+  const Columns<T, I, kFull> cols(l, G, dim);
+  const auto own = [&](int i, int j) { return kShort ? j < dim : cols.own(i, j); };
   float w[I * V], dw[I * V], db[I * V];
-  load_params<T, V, I>(w, a.weight, a.wide_weight, 1.0f, l, G, nvec);
+  load_params<T, I, kFull, kShort>(w, a.weight, a.wide_weight, 1.0f, cols, dim);
 #pragma unroll
   for (int e = 0; e < I * V; ++e) dw[e] = db[e] = 0.0f;
   const int sub = kBlock ? 0 : threadIdx.x / G;
-  Row<T, V, I> nx, ng;
   int64_t r = (int64_t)blockIdx.x * per + sub;
   const int64_t step = (int64_t)gridDim.x * per;
-  nx.load(static_cast<const T*>(a.x) + r * a.x_stride, l, G, nvec, r < a.n);
-  ng.load(static_cast<const T*>(a.grad) + r * a.grad_stride, l, G, nvec, r < a.n);
+  Raw nx[I] = {}, ng[I] = {};
+  const auto load = [&](int64_t row) {
+    if (row < a.n) {
+      load_row<T, I, kFull, kShort>(nx, static_cast<const T*>(a.x) + row * a.x_stride, cols, dim);
+      load_row<T, I, kFull, kShort>(ng, static_cast<const T*>(a.grad) + row * a.grad_stride, cols, dim);
+    }
+  };
+  if constexpr (kAhead) load(r);
   for (int64_t base = (int64_t)blockIdx.x * per; base < a.n; base += step, r += step) {
-    const Row<T, V, I> x = nx, g = ng;
-    const bool more = r + step < a.n;
-    nx.load(static_cast<const T*>(a.x) + (r + step) * a.x_stride, l, G, nvec, more);
-    ng.load(static_cast<const T*>(a.grad) + (r + step) * a.grad_stride, l, G, nvec, more);
+    if constexpr (!kAhead) load(r);
+    float x[I * V];
+    Raw gr[I];
     float s[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+    for (int i = 0; i < I; ++i) {
+      gr[i] = ng[i];
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[0] += (float)x.p[i].v[j];
+      for (int j = 0; j < V; ++j) {
+        x[i * V + j] = element<T>(nx[i], j);
+        s[0] += own(i, j) ? x[i * V + j] : 0.0f;
+      }
+    }
+    if constexpr (kAhead) load(r + step);
     row_sums<kBlock>(s, G, lds1);
     const float mean = s[0] * inv;
     float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < I; ++i)
-      if (i * G + l < nvec) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float d = (float)x.p[i].v[j] - mean, gw = (float)g.p[i].v[j] * w[i * V + j];
-          q[0] += d;
-          q[1] = __builtin_fmaf(d, d, q[1]);
-          q[2] += gw;
-          q[3] = __builtin_fmaf(gw, d, q[3]);
-        }
+      for (int j = 0; j < V; ++j) {
+        x[i * V + j] -= mean;
+        const float d = own(i, j) ? x[i * V + j] : 0.0f;
+        const float gw = own(i, j) ? element<T>(gr[i], j) * w[i * V + j] : 0.0f;
+        q[0] += d;
+        q[1] = __builtin_fmaf(d, d, q[1]);
+        q[2] += gw;
+        q[3] = __builtin_fmaf(gw, d, q[3]);
       }
     row_sums<kBlock>(q, G, lds2);
     const float off = q[0] * inv;
@@ -217,130 +268,157 @@ __global__ __launch_bounds__(kBlock ? kNormMaxThreads : kNormThreads) void k_lay
     if (r < a.n) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        const int v = i * G + l;
-        if (v < nvec) {
-          Pack<T, V> o;
+        LoosePack<T, V> o;
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const float h = (((float)x.p[i].v[j] - mean) - off) * rstd, dy = (float)g.p[i].v[j];
-            o.v[j] = (T)(rstd * (__builtin_fmaf(dy, w[i * V + j], -g_mean) - h * gh_mean));
-            dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
-            db[i * V + j] += dy;
-          }
-          if (a.out != nullptr)
-            *reinterpret_cast<Pack<T, V>*>(static_cast<T*>(a.out) + r * a.out_stride + (int64_t)v * V) = o;
+        for (int j = 0; j < V; ++j) {
+          const float h = (x[i * V + j] - off) * rstd, dy = element<T>(gr[i], j);
+          o.v[j] = (T)(rstd * (__builtin_fmaf(dy, w[i * V + j], -g_mean) - h * gh_mean));
+          dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
+          db[i * V + j] += dy;
         }
+        if (a.out != nullptr && (kFull || kShort || cols.skip[i] < V))
+          store_row<T, V, kShort>(static_cast<T*>(a.out) + r * a.out_stride, cols.at[i], dim, o);
       }
     }
   }
   if (a.sums == nullptr) return;
-  float* mine = a.sums + (int64_t)blockIdx.x * 2 * a.dim;
+  float* mine = a.sums + (int64_t)blockIdx.x * 2 * dim;
   if constexpr (kBlock) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (i * G + l) * V + j;
-        if (c < a.dim) {
-          mine[c] = dw[i * V + j];
-          mine[a.dim + c] = db[i * V + j];
+      for (int j = 0; j < V; ++j)
+        if (own(i, j)) {
+          mine[cols.at[i] + j] = dw[i * V + j];
+          mine[dim + cols.at[i] + j] = db[i * V + j];
         }
-      }
   } else {
+    // by nominal column: vector i of lane l begins at (i G + l) V, its own elements end it
     const int width = G * I * V;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < I; ++i)
+      for (int i = 0; i < I; ++i) {
+        const float* t = (which ? db : dw) + i * V;
 #pragma unroll
-        for (int j = 0; j < V; ++j) join[sub * width + (i * G + l) * V + j] = which ? db[i * V + j] : dw[i * V + j];
+        for (int e = 0; e < V; e += 4)
+          *reinterpret_cast<float4*>(join + sub * width + (i * G + l) * V + e) =
+              make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+      }
       __syncthreads();
-      for (int c = threadIdx.x; c < a.dim; c += kNormThreads) {
+      for (int c = threadIdx.x; c < dim; c += kNormThreads) {
+        // column c's place: in the last vector of the row the elements are at its end
+        const int first = c / V * V, at = kFull || kShort || first + V <= dim ? c : c + V - (dim - first);
         float t = 0.0f;
-        for (int k = 0; k < per; ++k) t += join[k * width + c];
-        mine[which * a.dim + c] = t;
+        for (int k = 0; k < per; ++k) t += join[k * width + at];
+        mine[which * dim + c] = t;
       }
     }
   }
 }
 
-// The blocks' sums to weight_grad and bias_grad: 64 columns a block, its waves
-// take every 16th block's sums, fp64 from here on.
-constexpr int kJoinSlices = 16;
+// The blocks' sums to weight_grad and bias_grad, fp64 from here on: 16 columns
+// (of both arrays) a block, a column's sums taken by 64 threads in turn.
+constexpr int kJoinCols = 16, kJoinSlices = 64;
 template <class T>
-__global__ __launch_bounds__(64 * kJoinSlices) void k_norm_join(const float* sums, int blocks, int dim, void* dw,
-                                                                void* db, bool wide) {
-  __shared__ double part[kJoinSlices][64];
-  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane;  // over both arrays
+__global__ __launch_bounds__(kJoinCols * kJoinSlices) void k_norm_join(const float* sums, int blocks, int dim, void* dw,
+                                                                       void* db, bool wide) {
+  __shared__ double part[kJoinSlices][kJoinCols];
+  const int col = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
+  const int c = blockIdx.x * kJoinCols + col;
   double t = 0.0;
   if (c < 2 * dim) {
-#pragma unroll 4
+#pragma unroll 8
     for (int b = slice; b < blocks; b += kJoinSlices) t += (double)sums[(int64_t)b * 2 * dim + c];
   }
-  part[slice][lane] = t;
+  part[slice][col] = t;
   __syncthreads();
-  if (slice != 0 || c >= 2 * dim) return;
-  for (int k = 1; k < kJoinSlices; ++k) t += part[k][lane];
+  if (slice >= 4) return;
+  t = 0.0;
+  for (int k = slice; k < kJoinSlices; k += 4) t += part[k][col];
+  t += __shfl_xor(t, kJoinCols);
+  t += __shfl_xor(t, 2 * kJoinCols);
   void* to = c < dim ? dw : db;
-  if (to == nullptr) return;
+  if (slice != 0 || c >= 2 * dim || to == nullptr) return;
   const int at = c < dim ? c : c - dim;
   if (wide) static_cast<float*>(to)[at] = (float)t;
   else static_cast<T*>(to)[at] = (T)(float)t;
 }
 
-// How a row lies on lanes. Vectors are as wide as widths, strides and
-// addresses allow, at most 16 bytes; a lane takes the smaller number of them
-// that leaves the row within a wave, else 16 elements.
+// How a row lies on lanes: one vector a lane where that leaves the row within
+// a wave, else 16 elements.
 struct NormPlan {
-  int V, I, G;
-  bool block;
+  int I, G;
+  bool block;  // a block a row
+  bool full;   // the lanes' vectors are the row, no more
 };
 
-NormPlan norm_plan(int dim, int size, std::initializer_list<const void*> ptrs, std::initializer_list<int64_t> strides) {
+// Blocks that the device holds at a time, and no call has more: a block takes
+// its rows in turn, and its columns of weight and bias once. (Each block of a
+// gradient also leaves 2 * dim floats of sums.)
+constexpr int kUnits = 256;
+int blocks_max(const NormPlan& p, bool grad) {
+  // waves a unit by the kernels' registers
+  const int threads = p.block ? p.G : kNormThreads;
+  const int waves = p.I == 1 ? (grad ? 20 : 32)
+                    : threads > kNormMidThreads || (grad && p.I == 2 && p.full && p.block) ? 16 : grad ? 12 : 20;
+  return kUnits * std::max(1, waves / (threads / 64));
+}
+
+// The rows in equal shares: the blocks of as many rounds as the most blocks
+// need. A gradient's blocks take at least kGradRows rows where that leaves a
+// block for each unit: a block's sums are written and read, 16 bytes a column
+// against 6 or 12 a row and column.
+constexpr int kGradRows = 8;
+int norm_blocks(const NormPlan& p, int64_t n, bool grad) {
+  const int64_t per = p.block ? 1 : kNormThreads / p.G, groups = (n + per - 1) / per;
+  int64_t most = blocks_max(p, grad);
+  if (grad) most = std::min(most, std::max<int64_t>(kUnits, n / kGradRows));
+  const int64_t rounds = (groups + most - 1) / most;
+  return (int)((groups + rounds - 1) / rounds);
+}
+
+NormPlan norm_plan(int dim, int size) {
   NormPlan p;
-  p.V = 16 / size;
-  while (p.V > 1 && (dim % p.V != 0 || !all_aligned((size_t)p.V * size, size, ptrs, strides))) p.V = p.V > 2 ? 2 : 1;
-  const int few = p.V == 8 ? 1 : p.V == 4 ? 1 : p.V == 2 ? 2 : 4, many = 16 / p.V;
-  const int nvec = dim / p.V;
-  p.block = false;
-  for (int i : {few, many}) {
+  const int V = 16 / size, nvec = (dim + V - 1) / V;
+  for (int i : {1, 16 / V}) {
     p.I = i;
     p.G = 1;
     while (p.G * i < nvec) p.G *= 2;
-    if (p.G <= 64) return p;
+    p.block = p.G > 64;
+    if (!p.block) break;
   }
-  p.block = true;
-  p.G = (nvec + p.I * 64 - 1) / (p.I * 64) * 64;
+  if (p.block) p.G = (nvec + p.I * 64 - 1) / (p.I * 64) * 64;
+  p.full = dim == p.G * p.I * V;
   return p;
 }
 
-template <class T, bool kGrad, int V, int I>
-hipError_t launch_norm(const NormPlan& p, const NormArgs& a, int blocks, hipStream_t st) {
-  const size_t lds = kGrad && !p.block && a.sums != nullptr ? sizeof(float) * kNormThreads * I * V : 0;
-  if constexpr (kGrad) {
-    if (p.block) hipLaunchKernelGGL((k_layer_norm_grad<T, V, I, true>), dim3(blocks), dim3(p.G), lds, st, a);
-    else hipLaunchKernelGGL((k_layer_norm_grad<T, V, I, false>), dim3(blocks), dim3(kNormThreads), lds, st, a);
-  } else {
-    if (p.block) hipLaunchKernelGGL((k_layer_norm<T, V, I, true>), dim3(blocks), dim3(p.G), 0, st, a);
-    else hipLaunchKernelGGL((k_layer_norm<T, V, I, false>), dim3(blocks), dim3(kNormThreads), 0, st, a);
-  }
-  return hipGetLastError();
-}
-
 template <class T, bool kGrad>
-hipError_t dispatch_norm(const NormPlan& p, const NormArgs& a, int blocks, hipStream_t st) {
-  constexpr int kFull = 16 / sizeof(T);
-  const bool many = p.I * p.V == 16;
-  if (p.V == kFull) {
-    return many ? launch_norm<T, kGrad, kFull, 16 / kFull>(p, a, blocks, st)
-                : launch_norm<T, kGrad, kFull, 1>(p, a, blocks, st);
-  }
-  if (p.V == 2) {
-    return many ? launch_norm<T, kGrad, 2, 8>(p, a, blocks, st) : launch_norm<T, kGrad, 2, 2>(p, a, blocks, st);
-  }
-  return many ? launch_norm<T, kGrad, 1, 16>(p, a, blocks, st) : launch_norm<T, kGrad, 1, 4>(p, a, blocks, st);
+hipError_t launch_norm(const NormPlan& p, const NormArgs& a, int blocks, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T), kMany = sizeof(T);  // vectors of 16 elements
+  const size_t lds = kGrad && !p.block && a.sums != nullptr ? sizeof(float) * kNormThreads * p.I * V : 0;
+  const dim3 grid(blocks), block(p.block ? p.G : kNormThreads);
+  const auto go = [&](auto i, auto most, auto full, auto shrt) {
+    constexpr int I = decltype(i)::value, kMost = decltype(most)::value;
+    constexpr bool kFull = decltype(full)::value, kShort = decltype(shrt)::value;
+    if constexpr (kGrad) hipLaunchKernelGGL((k_layer_norm_grad<T, I, kMost, kFull, kShort>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((k_layer_norm<T, I, kMost, kFull, kShort>), grid, block, lds, st, a);
+  };
+  using std::integral_constant;
+  using Yes = std::true_type;
+  using No = std::false_type;
+  const auto sized = [&](auto full) {
+    if (p.I == 1) go(integral_constant<int, 1>{}, integral_constant<int, 0>{}, full, No{});
+    else if (!p.block) go(integral_constant<int, kMany>{}, integral_constant<int, 0>{}, full, No{});
+    else if (p.G <= kNormMidThreads)
+      go(integral_constant<int, kMany>{}, integral_constant<int, kNormMidThreads>{}, full, No{});
+    else go(integral_constant<int, kMany>{}, integral_constant<int, kNormMaxThreads>{}, full, No{});
+  };
+  if (a.dim < V) go(integral_constant<int, 1>{}, integral_constant<int, 0>{}, No{}, Yes{});
+  else if (p.full) sized(Yes{});
+  else sized(No{});
+  return hipGetLastError();
 }
 
 int check_norm(const void* x, int64_t x_stride, int64_t n, int32_t dim, float eps, int dtype, int weight_dtype) {
@@ -375,7 +453,7 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (d_out == d_x && n > 1 && x_stride != out_stride)
     return op_error(MLKV_EINVAL, "out may be x only with the same stride");
-  const NormPlan p = norm_plan(dim, size, {d_x, d_out}, {x_stride, out_stride});
+  const NormPlan p = norm_plan(dim, size);
   NormArgs a{};
   a.x = d_x;
   a.weight = d_weight;
@@ -388,10 +466,9 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
   a.G = p.G;
   a.eps = eps;
   a.wide_weight = weight_dtype == MLKV_F32;
-  const int64_t per = p.block ? 1 : kNormThreads / p.G;
-  const int blocks = (int)std::min<int64_t>((n + per - 1) / per, 2048);
+  const int blocks = norm_blocks(p, n, false);
   const hipError_t e = dispatch_type(dtype, [&](auto t) {
-    return dispatch_norm<decltype(t), false>(p, a, blocks, static_cast<hipStream_t>(hip_stream));
+    return launch_norm<decltype(t), false>(p, a, blocks, static_cast<hipStream_t>(hip_stream));
   });
   return e == hipSuccess ? MLKV_OK : op_launch_error(e, "mlkv_layer_norm launch");
 }
@@ -399,7 +476,11 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
 int64_t mlkv_layer_norm_grad_workspace(int64_t n, int32_t dim) {
   if (n < 0 || n > 0x7FFFFFFFll) return op_error(MLKV_EINVAL, "n must be in [0, 2^31 - 1]");
   if (dim < 1 || dim > MLKV_NORM_MAX_DIM) return op_error(MLKV_EINVAL, "dim must be in [1, 16384]");
-  return (int64_t)sizeof(float) * 2 * dim * std::min<int64_t>(n, grad_blocks_max(dim));
+  if (n == 0) return 0;
+  // (the type is not known here: the most blocks of any)
+  int64_t blocks = 0;
+  for (int size : {2, 4}) blocks = std::max<int64_t>(blocks, norm_blocks(norm_plan(dim, size), n, true));
+  return (int64_t)sizeof(float) * 2 * dim * blocks;
 }
 
 int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight, const void* d_grad,
@@ -429,8 +510,7 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   int blocks = 0;
   if (n > 0) {
-    const NormPlan p = norm_plan(dim, size, {d_x, d_grad, d_x_grad},
-                                 {x_stride, grad_stride, d_x_grad != nullptr ? x_grad_stride : 0});
+    const NormPlan p = norm_plan(dim, size);
     NormArgs a{};
     a.x = d_x;
     a.grad = d_grad;
@@ -445,15 +525,15 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
     a.G = p.G;
     a.eps = eps;
     a.wide_weight = weight_dtype == MLKV_F32;
-    const int64_t per = p.block ? 1 : kNormThreads / p.G;
-    blocks = (int)std::min<int64_t>((n + per - 1) / per, grad_blocks_max(dim));
+    blocks = norm_blocks(p, n, true);
     const hipError_t e =
-        dispatch_type(dtype, [&](auto t) { return dispatch_norm<decltype(t), true>(p, a, blocks, st); });
+        dispatch_type(dtype, [&](auto t) { return launch_norm<decltype(t), true>(p, a, blocks, st); });
     if (e != hipSuccess) return op_launch_error(e, "mlkv_layer_norm_grad launch");
   }
   if (!sums) return MLKV_OK;
   const hipError_t e = dispatch_type(dtype, [&](auto t) {
-    hipLaunchKernelGGL((k_norm_join<decltype(t)>), dim3((2 * dim + 63) / 64), dim3(64 * kJoinSlices), 0, st,
+    hipLaunchKernelGGL((k_norm_join<decltype(t)>), dim3((2 * dim + kJoinCols - 1) / kJoinCols),
+                       dim3(kJoinCols * kJoinSlices), 0, st,
                        static_cast<const float*>(d_work), blocks, dim, d_weight_grad, d_bias_grad,
                        weight_dtype == MLKV_F32);
     return hipGetLastError();

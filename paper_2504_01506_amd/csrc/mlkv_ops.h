@@ -5,6 +5,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+#include <type_traits>
+
 #include "mlkv.h"
 
 namespace mlkv {
@@ -46,15 +49,43 @@ inline bool stride_ok(int64_t stride, int64_t rows, int64_t width, bool same) {
   return stride >= width && stride <= (int64_t(1) << 60) / rows;
 }
 
-// V elements of T as one load or store.
+// V elements of T as one load or store, at a multiple of its size ...
 template <class T, int V>
 struct __align__(sizeof(T) * V) Pack {
   T v[V];
 };
+// ... or at any address that T may have: the same 16-byte instruction, which
+// the memory pipeline takes at any alignment.
+template <class T, int V>
+struct __attribute__((packed, aligned(sizeof(T)))) LoosePack {
+  T v[V];
+};
+
+// 16 bytes in flight: whole registers, so that what is loaded is not unpacked,
+// and waited for, before it is used.
+using Raw = uint32_t __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(2))) LooseRaw {
+  Raw v;
+};
+__device__ __forceinline__ Raw load_raw(const void* p) { return static_cast<const LooseRaw*>(p)->v; }
+
+// Element j of 16 bytes of T.
+template <class T>
+__device__ __forceinline__ float element(const Raw& r, int j) {
+  if constexpr (sizeof(T) == 4) {
+    return __uint_as_float(r[j]);
+  } else if constexpr (std::is_same<T, bf16>::value) {
+    return __uint_as_float(j & 1 ? r[j >> 1] & 0xFFFF0000u : r[j >> 1] << 16);
+  } else {
+    const uint16_t h = (uint16_t)(j & 1 ? r[j >> 1] >> 16 : r[j >> 1]);
+    return (float)__builtin_bit_cast(f16, h);
+  }
+}
 
 // The sum of v over groups of G lanes (a power of two, at most 64), in every
 // lane of the group. All lanes of the wave must be active. Within 16 lanes by
-// data-parallel moves (xor 1, xor 2, then mirrors, which meet equal values).
+// data-parallel moves (xor 1, xor 2, then mirrors, which meet equal values),
+// then by exchanging rows of 16 and halves of the wave.
 template <int kCtrl>
 __device__ __forceinline__ float dpp_move(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, false));
@@ -64,8 +95,14 @@ __device__ __forceinline__ float group_sum(float v, int G) {
   if (G > 2) v += dpp_move<0x4E>(v);    // quad_perm 2 3 0 1
   if (G > 4) v += dpp_move<0x141>(v);   // row_half_mirror
   if (G > 8) v += dpp_move<0x140>(v);   // row_mirror
-  if (G > 16) v += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x401F));  // xor 16
-  if (G > 32) v += __shfl_xor(v, 32);
+  if (G > 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (G > 32) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
   return v;
 }
 

@@ -16,12 +16,15 @@ done; what a call allocates belongs to `stream`.
 """
 from __future__ import annotations
 
-import contextlib
 from typing import NamedTuple, Optional
 
 import torch
 
 from . import mlkv
+
+# a stream's handle without the Stream object around it (a microsecond and a half a call), where torch has that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 _TYPES = {torch.float32: mlkv.MLKV_F32, torch.bfloat16: mlkv.MLKV_BF16, torch.float16: mlkv.MLKV_F16}
 
@@ -61,14 +64,12 @@ def _rows(t: torch.Tensor, what: str) -> tuple[int, int, int]:
     if width == 0:
         raise ValueError(f"{what} has rows of no elements")
     n = t.numel() // width
-    if t.dim() == 1 or n <= 1:
-        if t.stride(-1) != 1 and width > 1:
-            raise ValueError(f"{what}: the elements of a row must lie next to each other")
+    if t.is_contiguous():
         return n, width, width
-    if n == 0:
-        return 0, width, width
     if t.stride(-1) != 1 and width > 1:
         raise ValueError(f"{what}: the elements of a row must lie next to each other")
+    if n <= 1:
+        return n, width, width
     stride = None
     for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
         if size == 1:
@@ -84,23 +85,36 @@ def _rows(t: torch.Tensor, what: str) -> tuple[int, int, int]:
 
 def _out(t: Optional[torch.Tensor], what: str, like: torch.Tensor) -> torch.Tensor:
     if t is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     _check(t, what, like, like.dtype, like.shape)
     return t
 
 
-@contextlib.contextmanager
-def _queue(t: torch.Tensor, stream):
-    """Makes the tensor's device current, and `stream` its current stream; yields the stream's handle."""
-    with torch.cuda.device(t.device):
-        if stream is None:
-            yield torch.cuda.current_stream().cuda_stream
-            return
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-        if s.device != t.device:
-            raise ValueError(f"the stream is of {s.device}, the tensors are on {t.device}")
-        with torch.cuda.stream(s):
-            yield s.cuda_stream
+class _Queue:
+    """Makes a tensor's device current, and `stream` its current stream; entered, gives the stream's handle.
+    Where both are so already nothing is changed (a call's host time counts in microseconds)."""
+    __slots__ = ("device", "stream", "held")
+
+    def __init__(self, t: torch.Tensor, stream):
+        self.device, self.stream, self.held = t.device, stream, None
+
+    def __enter__(self) -> int:
+        if self.stream is None and self.device.index == torch.cuda.current_device():
+            return _raw_stream(self.device.index)
+        s = self.stream
+        if s is None:
+            s = torch.cuda.current_stream(self.device)
+        elif isinstance(s, int):
+            s = torch.cuda.ExternalStream(s, device=self.device)
+        elif s.device != self.device:
+            raise ValueError(f"the stream is of {s.device}, the tensors are on {self.device}")
+        self.held = torch.cuda.stream(s)
+        self.held.__enter__()
+        return s.cuda_stream
+
+    def __exit__(self, *what):
+        if self.held is not None:
+            self.held.__exit__(*what)
 
 
 def _bytes(n: int) -> int:
@@ -109,19 +123,13 @@ def _bytes(n: int) -> int:
     return n
 
 
-def _params(x: torch.Tensor, dim: int, **params) -> int:
-    """Checks a weight and a bias (fp32 or of x's type, the same for both); their type's code."""
-    kind = None
-    for what, p in params.items():
-        if p is None:
-            continue
-        _check(p, what, x, shape=(dim,), dense=True)
-        if p.dtype not in (torch.float32, x.dtype):
-            raise ValueError(f"{what} must be float32 or {x.dtype}, not {p.dtype}")
-        if kind not in (None, p.dtype):
-            raise ValueError("weight and bias must be of one type")
-        kind = p.dtype
-    return _TYPES[kind or x.dtype]
+def _param(p: Optional[torch.Tensor], what: str, x: torch.Tensor, dim: int):
+    """Checks a weight or a bias: fp32 or of x's type."""
+    if p is None:
+        return
+    _check(p, what, x, None, (dim,), True)
+    if p.dtype != torch.float32 and p.dtype != x.dtype:
+        raise ValueError(f"{what} must be float32 or {x.dtype}, not {p.dtype}")
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -131,8 +139,13 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     _on_gpu(x, "x")
     kind = _dtype(x, "x")
     n, dim, step = _rows(x, "x")
-    wkind = _params(x, dim, weight=weight, bias=bias)
-    with _queue(x, stream) as st:
+    _param(weight, "weight", x, dim)
+    _param(bias, "bias", x, dim)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must be of one type")
+    p = weight if weight is not None else bias
+    wkind = kind if p is None else _TYPES[p.dtype]
+    with _Queue(x, stream) as st:
         out = _out(out, "out", x)
         ostep = _rows(out, "out")[2]
         mlkv._check(mlkv.mlkv_layer_norm(x, step, weight, bias, n, dim, eps, kind, wkind, out, ostep, st))
@@ -148,15 +161,15 @@ def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch
     _on_gpu(x, "x")
     kind = _dtype(x, "x")
     n, dim, step = _rows(x, "x")
-    wkind = _params(x, dim, weight=weight)
+    _param(weight, "weight", x, dim)
+    wkind = kind if weight is None else _TYPES[weight.dtype]
     _check(grad, "grad", x, x.dtype, x.shape)
     gstep = _rows(grad, "grad")[2]
-    with _queue(x, stream) as st:
+    with _Queue(x, stream) as st:
         out = _out(out, "out", x)
         ostep = _rows(out, "out")[2]
-        wtype = x.dtype if weight is None else weight.dtype
-        dw = torch.empty(dim, dtype=wtype, device=x.device)
-        db = torch.empty(dim, dtype=wtype, device=x.device)
+        dw = x.new_empty(dim) if weight is None else torch.empty_like(weight)
+        db = torch.empty_like(dw)
         nbytes = _bytes(mlkv.mlkv_layer_norm_grad_workspace(n, dim))
         work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
         mlkv._check(mlkv.mlkv_layer_norm_grad(x, step, weight, grad, gstep, n, dim, eps, kind, wkind, out, ostep, dw,
@@ -182,14 +195,13 @@ def log_probs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, stream=N
     lead = logits.shape[:-1]
     _check(tokens, "tokens", logits, torch.int64, lead, dense=True)
     top = int(top)
-    with _queue(logits, stream) as st:
+    with _Queue(logits, stream) as st:
         nbytes = _bytes(mlkv.mlkv_log_probs_workspace(n, vocab, top, kind))
 
-        def new(*tail, dtype=torch.float32):
-            return torch.empty((*lead, *tail), dtype=dtype, device=logits.device)
-
-        r = LogProbs(new(), new(), new(2), new(top, dtype=torch.int64) if top else None, new(top) if top else None)
-        work = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+        logp = torch.empty(lead, dtype=torch.float32, device=logits.device)
+        r = LogProbs(logp, torch.empty_like(logp), logp.new_empty((*lead, 2)),
+                     tokens.new_empty((*lead, top)) if top else None, logp.new_empty((*lead, top)) if top else None)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=logits.device) if nbytes else None
         mlkv._check(mlkv.mlkv_log_probs(logits, step, tokens, n, vocab, top, kind, r.logp, r.entropy, r.stats,
                                         r.top_ids, r.top_logp, work, nbytes, st))
     return r
@@ -218,7 +230,7 @@ def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: 
             raise ValueError("entropy_grad needs entropy")
     if entropy is not None:
         _check(entropy, "entropy", logits, torch.float32, lead, dense=True)
-    with _queue(logits, stream) as st:
+    with _Queue(logits, stream) as st:
         out = _out(out, "out", logits)
         ostep = _rows(out, "out")[2]
         mlkv._check(mlkv.mlkv_log_probs_grad(logits, step, tokens, stats, entropy, logp_grad, entropy_grad, n, vocab,
@@ -253,7 +265,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
     batch = g.shape[0] if g.dim() == 3 else 1
     rows, cols = g.shape[-2:]
     gb, gr = _matrices(g, "g")
-    with _queue(g, stream) as st:
+    with _Queue(g, stream) as st:
         out = _out(out, "out", g)
         ob, orow = _matrices(out, "out")
         nbytes = _bytes(mlkv.mlkv_orthogonalize_workspace(batch, rows, cols))
