@@ -4,14 +4,16 @@
 // A row is cut into chunks, a block each, that hold their logits in registers:
 // every logit is read once. A thread sums e = exp(x - m) and e (x - m) against
 // the largest logit m of its own, and the joins (lanes, waves, chunks) rescale
-// to the larger of two maxima, the running softmax. A second kernel joins a
-// row's chunks, if there are several. Bound by HBM: about 12 operations a
-// logit, one of them an exponential, against 2 or 4 bytes.
+// to the largest of all, the running softmax. A second kernel joins a row's
+// chunks; where there are rows enough for the device, a block takes a row's
+// chunks in turn instead, and rows of few logits are a wave each. Bound by
+// HBM: 9 operations a logit, one of them an exponential (of the rate of four),
+// against 2 or 4 bytes.
 //
-// Alternatives are ordered by one 64-bit key of value and index, so that equal
-// logits have an order and no two keys are equal. The k-th largest of the
-// threads' own largest keys is a bound that the row's k largest reach, and at
-// most k threads reach it: only their few logits are ranked.
+// Alternatives: a chunk leaves the largest logit of each group of 16 vectors.
+// A row's k largest logits are in the k groups whose largest are (equal ones
+// in the order of their indices, which is that of the groups), so only those
+// groups are read again, 1 of 250 for k = 4 and 128,000 logits.
 #include "mlkv_ops.h"
 
 #include <algorithm>
@@ -21,6 +23,7 @@ namespace {
 
 constexpr int kChunkThreads = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff();
 
 // Sums of a part of a row: m its largest logit, s = sum 2^z, t = sum z 2^z
@@ -29,32 +32,46 @@ struct Part {
   float m, s, t, pad;
 };
 
-__device__ __forceinline__ Part part_join(const Part& a, const Part& b) {
+// The part's sums against a larger maximum (or its own).
+__device__ __forceinline__ Part part_scale(const Part& p, float m) {
   Part r;
-  r.m = fmaxf(a.m, b.m);
-  // a part of -inf alone has nothing to rescale
-  const float da = a.m == -kInf ? 0.0f : (a.m - r.m) * kLog2e;
-  const float db = b.m == -kInf ? 0.0f : (b.m - r.m) * kLog2e;
-  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-  r.s = fa * a.s + fb * b.s;
-  // (2^z is 0 long before z leaves the range in which z 2^z is 0)
-  r.t = fa * __builtin_fmaf(fmaxf(da, -1e4f), a.s, a.t) + fb * __builtin_fmaf(fmaxf(db, -1e4f), b.s, b.t);
+  const float d = p.m == -kInf ? 0.0f : (p.m - m) * kLog2e;  // (-inf alone: nothing to rescale)
+  const float f = __builtin_amdgcn_exp2f(d);
+  r.m = m;
+  r.s = f * p.s;
+  // (2^d is 0 long before d leaves the range in which d 2^d is 0)
+  r.t = f * __builtin_fmaf(fmaxf(d, -1e4f), p.s, p.t);
   r.pad = 0.0f;
   return r;
 }
-
-__device__ __forceinline__ Part wave_join(Part p) {
+__device__ __forceinline__ Part part_join(const Part& a, const Part& b) {
+  const float m = fmaxf(a.m, b.m);
+  Part x = part_scale(a, m);
+  const Part y = part_scale(b, m);
+  x.s += y.s;
+  x.t += y.t;
+  return x;
+}
+// ... of a wave's lanes, in every lane; a block's from its waves'.
+__device__ __forceinline__ Part wave_join(const Part& p) {
+  Part r = part_scale(p, wave_max(p.m));
+  r.s = group_sum(r.s, 64);
+  r.t = group_sum(r.t, 64);
+  return r;
+}
+template <int kWaves>
+__device__ __forceinline__ Part waves_join(const Part* p) {
+  float m = p[0].m;
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    Part q;
-    q.m = __shfl_xor(p.m, o);
-    q.s = __shfl_xor(p.s, o);
-    q.t = __shfl_xor(p.t, o);
-    q.pad = 0.0f;
-    // the lower lane's part first on both sides: equal bits in every lane
-    p = (threadIdx.x & o) ? part_join(q, p) : part_join(p, q);
+  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, p[w].m);
+  Part r = part_scale(p[0], m);
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    const Part x = part_scale(p[w], m);
+    r.s += x.s;
+    r.t += x.t;
   }
-  return p;
+  return r;
 }
 
 // Order of logits as unsigned numbers; -0 counts as +0. Every logit's is over 0.
@@ -65,10 +82,11 @@ __device__ __forceinline__ uint32_t value_key(float x) {
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-// value, then lowest index first
+// value, then lowest index first; 0 for a NaN, as for what is not there
 __device__ __forceinline__ uint64_t full_key(float x, uint32_t i) {
-  return (uint64_t)value_key(x) << 32 | (uint32_t)~i;
+  return x == x ? (uint64_t)value_key(x) << 32 | (uint32_t)~i : 0;
 }
+__device__ __forceinline__ uint32_t key_index(uint64_t k) { return ~(uint32_t)k; }
 
 struct LogpArgs {
   const void* logits;
@@ -79,10 +97,14 @@ struct LogpArgs {
   int64_t* top_ids;
   float* top_logp;
   Part* parts;            // [n][chunks]
-  uint64_t* keys;         // [n][chunks][top], largest first; 0 where a chunk has fewer
+  uint32_t* groups;       // [n][chunks][kGroups * L] value keys of the groups' largest logits
   int64_t stride, n;
   int vocab, top, chunks;
+  int chunk_groups;       // kGroups * L
 };
+
+constexpr int kGroupVecs = 16;                          // vectors of a group: lanes that a DPP row joins
+constexpr int kGroups = kChunkThreads / kGroupVecs;     // groups of a chunk, for each vector of a thread
 
 // What a row's sums give.
 struct RowStats {
@@ -99,34 +121,41 @@ __device__ __forceinline__ RowStats row_stats(const Part& p) {
   } else if (!(p.s < kInf)) {  // a NaN or +inf
     r.m = r.logs = r.ent = __builtin_nanf("");
   } else {
-    const double s = (double)p.s, l = log(s);
     r.m = p.m;
-    r.logs = (float)l;
-    r.ent = (float)(l - (double)p.t * 0.693147180559945309417 / s);
+    r.logs = logf(p.s);
+    r.ent = r.logs - p.t * kLn2 / p.s;  // (t <= 0: nothing cancels)
   }
   return r;
 }
 
 __device__ __forceinline__ float log_prob(float x, const RowStats& r) { return r.none ? -kInf : (x - r.m) - r.logs; }
 
+// The row's token and its logit, loaded by the thread that writes them, well before.
+struct Given {
+  int64_t token;
+  float logit;
+};
 template <class T>
-__device__ __forceinline__ void write_row(const LogpArgs& a, int64_t row, const RowStats& r) {
+__device__ __forceinline__ Given given(const LogpArgs& a, int64_t row, const T* x) {
+  Given g = {-1, 0.0f};
+  if (a.logp != nullptr) g.token = a.tokens[row];
+  if (g.token >= 0 && g.token < a.vocab) g.logit = (float)x[g.token];
+  return g;
+}
+
+__device__ __forceinline__ void write_row(const LogpArgs& a, int64_t row, const RowStats& r, const Given& g) {
   if (a.stats != nullptr) {
     a.stats[2 * row] = r.m;
     a.stats[2 * row + 1] = r.logs;
   }
   if (a.entropy != nullptr) a.entropy[row] = r.ent;
   if (a.logp != nullptr) {
-    const int64_t t = a.tokens[row];
-    float lp = 0.0f;
-    if (t >= a.vocab) lp = __builtin_nanf("");
-    else if (t >= 0) lp = log_prob((float)static_cast<const T*>(a.logits)[row * a.stride + t], r);
-    a.logp[row] = lp;
+    a.logp[row] = g.token >= a.vocab ? __builtin_nanf("") : g.token < 0 ? 0.0f : log_prob(g.logit, r);
   }
 }
 
 __device__ __forceinline__ void write_top(const LogpArgs& a, int64_t row, int rank, uint64_t key, const RowStats& r) {
-  if (a.top_ids != nullptr) a.top_ids[row * a.top + rank] = r.m != r.m ? -1 : (int64_t)(uint32_t)~(uint32_t)key;
+  if (a.top_ids != nullptr) a.top_ids[row * a.top + rank] = r.m != r.m ? -1 : (int64_t)key_index(key);
   if (a.top_logp != nullptr) a.top_logp[row * a.top + rank] = log_prob(key_value((uint32_t)(key >> 32)), r);
 }
 
@@ -144,245 +173,417 @@ struct Cut {
   }
 };
 
-// One chunk of a row: L vectors a thread.
-template <class T, int L, bool kTop>
+// ---- the k largest keys of a team (a wave or a block) ----
+// The k-th largest of the threads' (of a block: of every four threads') largest
+// values, cut to 16 bits, is a bound that the k largest reach; the keys over
+// it, hardly more than k, are ranked by counting. Many equal values can leave
+// more than kCands of them: then the bound is the k-th largest of the threads'
+// own largest keys, which no more than k threads reach, and where even those
+// hold too many (large ones in few threads), the largest key below the last is
+// sought k times.
+template <int kTeam>
+struct Select {
+  static constexpr int kCands = kTeam == 64 ? 512 : 1024;
+  uint32_t quad[64];
+  uint64_t list[kTeam];
+  uint64_t cand[kCands];
+  uint64_t out[MLKV_LOGITS_MAX_TOP];  // largest first
+  uint64_t bound;
+  int listed, cands;
+};
+
+template <int kTeam>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (kTeam > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+// How many of p[0 .. n) are larger than f.
+__device__ __forceinline__ int count_over(const uint64_t* p, int n, uint64_t f) {
+  int over = 0, i = 0;
+  for (; i + 8 <= n; i += 8)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) over += p[i + e] > f;
+  for (; i < n; ++i) over += p[i] > f;
+  return over;
+}
+
+// each(f) calls f with every key of the thread: no two equal in the team, but
+// for 0, which does not count. q: the largest one's value. Returns how many of
+// the k there are, the same in all threads; s.out is ready for all.
+template <int kTeam, class Each>
+__device__ __forceinline__ int select_top(Select<kTeam>& s, int tid, uint32_t q, int k, const Each& each) {
+  constexpr int kCands = Select<kTeam>::kCands;
+  const int lane = tid & 63;
+  if constexpr (kTeam > 64) {
+    uint32_t t = max(q, dpp_bits<0xB1>(q));
+    t = max(t, dpp_bits<0x4E>(t));
+    if ((lane & 3) == 0) s.quad[tid >> 2] = t;
+  }
+  if (tid == 0) s.listed = s.cands = 0;
+  team_sync<kTeam>();
+  const uint32_t seen = kTeam > 64 ? s.quad[lane] : q;
+  uint32_t low = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t t = low | 1u << bit;
+    if (__popcll(__ballot(seen >= t)) >= k) low = t;
+  }
+  const auto collect = [&](uint64_t least) {
+    each([&](uint64_t f) {
+      if (f < least) return;
+      const int at = atomicAdd(&s.cands, 1);
+      if (at < kCands) s.cand[at] = f;
+    });
+  };
+  // (a key is at least its value's, and 1 where it counts)
+  if (q >= low && q != 0) collect((uint64_t)low << 32 | 1);
+  team_sync<kTeam>();
+  int nc = s.cands;
+  if (nc > kCands) {
+    uint64_t best = 0;
+    each([&](uint64_t f) { best = max(best, f); });
+    team_sync<kTeam>();
+    if (best != 0) s.list[atomicAdd(&s.listed, 1)] = best;
+    if (tid == 0) {
+      s.cands = 0;
+      s.bound = 1;  // (fewer than k threads have keys: all of those count)
+    }
+    team_sync<kTeam>();
+    const int nl = s.listed;
+    if (best != 0 && count_over(s.list, nl, best) == k - 1) s.bound = best;
+    team_sync<kTeam>();
+    if (best >= s.bound) collect(s.bound);
+    team_sync<kTeam>();
+    nc = s.cands;
+  }
+  if (nc <= kCands) {
+    for (int i = tid; i < nc; i += kTeam) {
+      const uint64_t f = s.cand[i];
+      const int over = count_over(s.cand, nc, f);
+      if (over < k) s.out[over] = f;
+    }
+    team_sync<kTeam>();
+    return min(nc, k);
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    uint64_t m = 0;
+    each([&](uint64_t f) {
+      if (f < last) m = max(m, f);
+    });
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) m = max(m, (uint64_t)__shfl_xor((unsigned long long)m, o));
+    if constexpr (kTeam > 64) {
+      if (lane == 0) s.list[tid >> 6] = m;
+      __syncthreads();
+      m = max(max(s.list[0], s.list[1]), max(s.list[2], s.list[3]));
+      __syncthreads();
+    }
+    if (tid == 0) s.out[r] = m;
+    last = m;
+  }
+  team_sync<kTeam>();
+  return k;  // (there are more than kCands)
+}
+
+// ... of the keys key(i), i < n, thread i % kTeam's.
+template <int kTeam, class Key>
+__device__ __forceinline__ int select_of(Select<kTeam>& s, int tid, int n, int k, const Key& key) {
+  constexpr int kHeld = 4;  // keys of a thread that are made once; the others for each look at them, as many at a time
+  const auto some = [&](int from, uint64_t (&f)[kHeld]) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f[j] = from + j * kTeam < n ? key(from + j * kTeam) : 0;
+  };
+  uint64_t held[kHeld], more[kHeld], best = 0;
+  some(tid, held);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) best = max(best, held[j]);
+#pragma unroll 1
+  for (int i = tid + kHeld * kTeam; i < n; i += kHeld * kTeam) {
+    some(i, more);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) best = max(best, more[j]);
+  }
+  return select_top<kTeam>(s, tid, (uint32_t)(best >> 32), k, [&](const auto& f) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f(held[j]);
+#pragma unroll 1
+    for (int i = tid + kHeld * kTeam; i < n; i += kHeld * kTeam) {
+      some(i, more);
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) f(more[j]);
+    }
+  });
+}
+static_assert(kChunkThreads == 256, "select_top's slow way joins four waves");
+
+// The k largest logits of a row from its groups' largest (in LDS or global memory).
+template <class T>
+__device__ __forceinline__ int select_logits(Select<kChunkThreads>& s, int tid, const T* x, const Cut<T>& cut,
+                                             const uint32_t* groups, int k, uint32_t* chosen) {
+  constexpr int V = 16 / sizeof(T), kSize = kGroupVecs * V;
+  const int ng = (cut.vecs + kGroupVecs - 1) / kGroupVecs;
+  const int nsel = select_of<kChunkThreads>(s, tid, ng, k, [&](int i) { return (uint64_t)groups[i] << 32 | (uint32_t)~i; });
+  if (tid < nsel) chosen[tid] = key_index(s.out[tid]);
+  __syncthreads();
+  // their logits, and those before and behind the vectors
+  const int inside = nsel * kSize, all = inside + cut.head + cut.tail, end = cut.head + cut.vecs * V;
+  return select_of<kChunkThreads>(s, tid, all, k, [&](int i) {
+    const int in = i < inside ? cut.head + (int)chosen[i / kSize] * kSize + i % kSize : end;
+    const int beside = i - inside < cut.head ? i - inside : end + (i - inside - cut.head);
+    const bool is = i >= inside || in < end;  // (the row's last group may be short)
+    const int at = i >= inside ? beside : min(in, end - 1);
+    const uint64_t f = full_key((float)x[at], (uint32_t)at);
+    return is ? f : 0;
+  });
+}
+
+// A thread's sums of L vectors and one more logit. vm: the vectors' largest.
+template <class T, int L>
+__device__ __forceinline__ Part thread_part(const Raw (&p)[L], float ex, float (&vm)[L]) {
+  constexpr int V = 16 / sizeof(T);
+  Part mine;
+  float m = ex;
+#pragma unroll
+  for (int j = 0; j < L; ++j) {
+    vm[j] = -kInf;
+#pragma unroll
+    for (int e = 0; e < V; ++e) vm[j] = fmaxf(vm[j], element<T>(p[j], e));
+    m = fmaxf(m, vm[j]);
+  }
+  if (m != m) m = -kInf;  // (a lone NaN)
+  const float base = m == -kInf ? 0.0f : m;
+  mine.m = m;
+  mine.pad = 0.0f;
+  // z = x log2(e) - m log2(e) in one operation; what the product's rounding
+  // shifts every z by (at most 2^-24 |m|) comes off the sums, to first order.
+  // Where that is not small, or a logit is -inf and t no number, the sums are
+  // taken again by steps.
+  const float c = base * kLog2e;
+  const float shift = __builtin_fmaf(base, kLog2e, -c);
+  mine.s = mine.t = 0.0f;
+#pragma unroll
+  for (int j = 0; j < L; ++j)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float z = __builtin_fmaf(element<T>(p[j], e), kLog2e, -c), q = __builtin_amdgcn_exp2f(z);
+      mine.s += q;
+      mine.t = __builtin_fmaf(q, z, mine.t);
+    }
+  mine.s = __builtin_fmaf(mine.s, -shift * kLn2, mine.s);
+  mine.t = __builtin_fmaf(mine.t, -shift * kLn2, mine.t) - shift * mine.s;
+  if (!(fabsf(mine.t) < kInf) || !(fabsf(shift) <= 0x1p-12f)) {
+    mine.s = mine.t = 0.0f;
+#pragma unroll
+    for (int j = 0; j < L; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float z = (element<T>(p[j], e) - base) * kLog2e, q = __builtin_amdgcn_exp2f(z);
+        mine.s += q;
+        mine.t = __builtin_fmaf(q, fmaxf(z, -150.0f), mine.t);
+      }
+  }
+  const float z = (ex - base) * kLog2e, q = __builtin_amdgcn_exp2f(z);
+  mine.s += q;
+  mine.t = __builtin_fmaf(q, fmaxf(z, -150.0f), mine.t);
+  return mine;
+}
+
+// The value keys of the groups of a chunk, from its vectors' largest logits:
+// lane j of a group writes that of the group of vector j.
+template <int L>
+__device__ __forceinline__ void group_maxima(const float (&vm)[L], uint32_t* to, int tid) {
+  const int lane = tid & (kGroupVecs - 1);
+  uint32_t mine = 0;
+#pragma unroll
+  for (int j = 0; j < L; ++j) {
+    uint32_t g = value_key(vm[j]);
+    g = max(g, dpp_bits<0xB1>(g));
+    g = max(g, dpp_bits<0x4E>(g));
+    g = max(g, dpp_bits<0x141>(g));
+    g = max(g, dpp_bits<0x140>(g));
+    if (lane == j) mine = g;
+  }
+  if (lane < L) to[lane * kGroups + tid / kGroupVecs] = mine;
+}
+
+// The thread's vectors, -inf where the row has none.
+template <class T, int L>
+__device__ __forceinline__ void load_vecs(Raw (&p)[L], const T* body, int first, int step, int vecs) {
+  constexpr int V = 16 / sizeof(T);
+  constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, bf16>::value ? 0xFF80FF80u : 0xFC00FC00u;
+#pragma unroll
+  for (int j = 0; j < L; ++j) {
+    const int v = first + j * step;
+    p[j] = Raw{kNone, kNone, kNone, kNone};
+    if (v < vecs) p[j] = load_raw(body + (int64_t)v * V);
+  }
+}
+
+// One chunk of a row: L vectors a thread. kTop: the alternatives are not
+// wanted, left to the join, or taken from this chunk, the row's only one.
+enum Top : int { kNoTop, kLeaveTop, kTakeTop };
+template <class T, int L, int kTop>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_chunk(LogpArgs a) {
   constexpr int V = 16 / sizeof(T), kWaves = kChunkThreads / 64;
   __shared__ Part wave_part[kWaves];
-  __shared__ uint32_t quad_key[64];
-  __shared__ uint64_t list[kChunkThreads];
-  __shared__ uint64_t bound;
-  __shared__ int listed, cands;
-  extern __shared__ uint64_t cand[];  // [top * (L * V + 1)]
+  __shared__ uint32_t group_max[kTop == kTakeTop ? kGroups * L : 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x / (uint32_t)a.chunks;
   const int chunk = (int)(blockIdx.x % (uint32_t)a.chunks);
   const T* x = static_cast<const T*>(a.logits) + row * a.stride;
   const Cut<T> cut(x, a.vocab);
-  const T* body = x + cut.head;
-  const int first = chunk * L * kChunkThreads + tid;  // the thread's vectors: first + j * kChunkThreads
-  Pack<T, V> p[L];
-#pragma unroll
-  for (int j = 0; j < L; ++j) {
-    const int v = first + j * kChunkThreads;
-    if (v < cut.vecs) {
-      p[j] = *reinterpret_cast<const Pack<T, V>*>(body + (int64_t)v * V);
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) p[j].v[e] = (T)-kInf;
-    }
-  }
-  // the first chunk takes the elements before the vectors, the last those behind, one a thread
-  int extra = -1;
+  Given token;
+  if (tid == 0 && a.chunks == 1) token = given(a, row, x);
+  Raw p[L];
+  load_vecs<T, L>(p, x + cut.head, chunk * L * kChunkThreads + tid, kChunkThreads, cut.vecs);
+  // the first chunk takes the logits before the vectors, the last those behind, one a thread
   float ex = -kInf;
-  if (chunk == 0 && tid < cut.head) extra = tid;
-  if (chunk == a.chunks - 1 && tid >= V && tid < V + cut.tail) extra = cut.head + cut.vecs * V + tid - V;
-  if (extra >= 0) ex = (float)x[extra];
-
-  if constexpr (kTop) {
-    if (tid == 0) listed = cands = 0;
-  }
-  float vm[L], m = ex;
-#pragma unroll
-  for (int j = 0; j < L; ++j) {
-    vm[j] = -kInf;
-#pragma unroll
-    for (int e = 0; e < V; ++e) vm[j] = fmaxf(vm[j], (float)p[j].v[e]);
-    m = fmaxf(m, vm[j]);
-  }
-  if (m != m) m = -kInf;  // (a lone NaN)
-  const float base = m == -kInf ? 0.0f : m;
-  Part mine;
-  mine.m = m;
-  mine.pad = 0.0f;
-  {
-    const float z = (ex - base) * kLog2e, q = __builtin_amdgcn_exp2f(z);
-    mine.s = q;
-    mine.t = q * fmaxf(z, -150.0f);
-  }
-#pragma unroll
-  for (int j = 0; j < L; ++j)
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float z = ((float)p[j].v[e] - base) * kLog2e, q = __builtin_amdgcn_exp2f(z);
-      mine.s += q;
-      mine.t = __builtin_fmaf(q, fmaxf(z, -150.0f), mine.t);  // (z may be -inf)
-    }
-  const Part joined = wave_join(mine);
+  if (chunk == 0 && tid < cut.head) ex = (float)x[tid];
+  if (chunk == a.chunks - 1 && tid >= V && tid < V + cut.tail) ex = (float)x[cut.head + cut.vecs * V + tid - V];
+  float vm[L];
+  const Part joined = wave_join(thread_part<T, L>(p, ex, vm));
   if (lane == 0) wave_part[tid >> 6] = joined;
-
-  const bool owns = first < cut.vecs || extra >= 0;
-  if constexpr (kTop) {
-    // a value that at least `top` threads reach, from the largest of every four threads
-    uint32_t k = owns ? value_key(m) : 0;
-    k = max(k, (uint32_t)__shfl_xor((int)k, 1));
-    k = max(k, (uint32_t)__shfl_xor((int)k, 2));
-    if ((lane & 3) == 0) quad_key[tid >> 2] = k;
+  if constexpr (kTop != kNoTop) {
+    group_maxima<L>(vm, kTop == kTakeTop ? group_max : a.groups + (row * a.chunks + chunk) * (kGroups * L), tid);
   }
   __syncthreads();
-  Part all = wave_part[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) all = part_join(all, wave_part[w]);
-
-  uint64_t best = 0;
-  int nc = 0;
-  if constexpr (kTop) {
-    const uint32_t q = quad_key[lane];
-    uint32_t low = 0;
-#pragma unroll 1
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t t = low | 1u << bit;
-      if (__popcll(__ballot(q >= t)) >= a.top) low = t;
-    }
-    // the first of a thread's largest logits, for the threads that reach it
-    const bool reach = owns && value_key(m) >= low;
-    if (__any(reach)) {
-      uint32_t at = 0xFFFFFFFFu;
-      if (extra >= 0 && ex == m) at = (uint32_t)extra;
-#pragma unroll
-      for (int j = L - 1; j >= 0; --j) {
-        const int v = first + j * kChunkThreads;
-        if (reach && v < cut.vecs && vm[j] == m) {
-#pragma unroll
-          for (int e = V - 1; e >= 0; --e)
-            if ((float)p[j].v[e] == m && !(extra >= 0 && extra < cut.head && ex == m))
-              at = (uint32_t)(cut.head + v * V + e);
-        }
-      }
-      if (reach && at != 0xFFFFFFFFu) {
-        best = full_key(m, at);
-        list[atomicAdd(&listed, 1)] = best;
-      }
-    }
-    __syncthreads();
-    // the top-th largest of them: no more than `top` threads hold keys as large
-    const int nl = listed;
-    if (best != 0) {
-      int over = 0;
-      for (int i = 0; i < nl; ++i) over += list[i] > best;
-      if (over == a.top - 1) bound = best;
-    }
-    if (nl < a.top && tid == 0) bound = 0;  // fewer threads have logits: all of those count
-    __syncthreads();
-    const uint64_t least = bound;
-    if (best != 0 && best >= least) {
-      const float lv = least ? key_value((uint32_t)(least >> 32)) : -kInf;
-      if (extra >= 0 && ex >= lv) {
-        const uint64_t f = full_key(ex, (uint32_t)extra);
-        if (f >= least) cand[atomicAdd(&cands, 1)] = f;
-      }
-#pragma unroll
-      for (int j = 0; j < L; ++j) {
-        const int v = first + j * kChunkThreads;
-        if (v < cut.vecs && vm[j] >= lv) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const uint64_t f = full_key((float)p[j].v[e], (uint32_t)(cut.head + v * V + e));
-            if (f >= least && !((float)p[j].v[e] != (float)p[j].v[e])) cand[atomicAdd(&cands, 1)] = f;
-          }
-        }
-      }
-    }
-    __syncthreads();
-    nc = cands;
-  }
-  if (a.chunks == 1) {
-    const RowStats r = row_stats(all);
-    if (tid == 0) write_row<T>(a, row, r);
-    if constexpr (kTop) {
-      for (int i = tid; i < nc; i += kChunkThreads) {
-        const uint64_t f = cand[i];
-        int over = 0;
-        for (int o = 0; o < nc; ++o) over += cand[o] > f;
-        if (over < a.top) write_top(a, row, over, f, r);
-      }
-      // (fewer keys than alternatives only where NaNs took their places)
-      for (int i = nc + tid; i < a.top; i += kChunkThreads) write_top(a, row, i, 0, r);
-    }
-  } else {
+  const Part all = waves_join<kWaves>(wave_part);
+  if (a.chunks > 1) {
     if (tid == 0) a.parts[row * a.chunks + chunk] = all;
-    if constexpr (kTop) {
-      uint64_t* to = a.keys + (row * a.chunks + chunk) * a.top;
-      for (int i = tid; i < nc; i += kChunkThreads) {
-        const uint64_t f = cand[i];
-        int over = 0;
-        for (int o = 0; o < nc; ++o) over += cand[o] > f;
-        if (over < a.top) to[over] = f;
-      }
-      for (int i = nc + tid; i < a.top; i += kChunkThreads) to[i] = 0;
-    }
+    return;
+  }
+  const RowStats r = row_stats(all);
+  if (tid == 0) write_row(a, row, r, token);
+  if constexpr (kTop == kTakeTop) {
+    __shared__ Select<kChunkThreads> sel;
+    __shared__ uint32_t chosen[MLKV_LOGITS_MAX_TOP];
+    const int found = select_logits<T>(sel, tid, x, cut, group_max, a.top, chosen);
+    // (fewer keys than alternatives only where NaNs took their places)
+    if (tid < a.top) write_top(a, row, tid, tid < found ? sel.out[tid] : 0, r);
   }
 }
 
-// Joins a row's chunks: a block a row. The bound on the alternatives: of the
-// chunks' keys number d the r-th largest, with r (d + 1) >= top keys as large.
-constexpr int kJoinThreads = 256;
-inline size_t join_lds(int chunks, int top) {
-  return sizeof(uint64_t) * ((size_t)chunks + (size_t)top * (std::min(chunks, top) + 1));
-}
+// Joins a row's chunks: a block a row.
 template <class T>
-__global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a) {
-  constexpr int kWaves = kJoinThreads / 64;
+__global__ __launch_bounds__(kChunkThreads) void k_logp_join(LogpArgs a) {
+  constexpr int kWaves = kChunkThreads / 64;
   __shared__ Part wave_part[kWaves];
-  __shared__ uint64_t bound;
-  __shared__ int cands;
-  extern __shared__ uint64_t lds[];
-  uint64_t* head = lds;              // [chunks]
-  uint64_t* cand = lds + a.chunks;   // [top * (min(chunks, top) + 1)]
+  __shared__ Select<kChunkThreads> sel;
+  __shared__ uint32_t chosen[MLKV_LOGITS_MAX_TOP];
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+  const Part* parts = a.parts + row * a.chunks;
+  Given token;
+  if (tid == 0) token = given(a, row, x);
   Part mine;
   mine.m = -kInf;
   mine.s = mine.t = mine.pad = 0.0f;
-  for (int c = tid; c < a.chunks; c += kJoinThreads) mine = part_join(mine, a.parts[row * a.chunks + c]);
+  if (tid < a.chunks) mine = parts[tid];
+  int found = 0;
+  if (a.top > 0) {
+    const Cut<T> cut(x, a.vocab);
+    found = select_logits<T>(sel, tid, x, cut, a.groups + row * a.chunks * a.chunk_groups, a.top, chosen);
+  }
+  for (int c = tid + kChunkThreads; c < a.chunks; c += kChunkThreads) mine = part_join(mine, parts[c]);
   mine = wave_join(mine);
   if ((tid & 63) == 0) wave_part[tid >> 6] = mine;
-  const uint64_t* keys = a.keys + row * a.chunks * a.top;
-  const int depth = a.top ? (a.top + a.chunks - 1) / a.chunks - 1 : 0;
-  const int need = a.top ? (a.top + depth) / (depth + 1) : 0;  // <= chunks
-  if (a.top) {
-    for (int c = tid; c < a.chunks; c += kJoinThreads) head[c] = keys[(int64_t)c * a.top + depth];
-    if (tid == 0) {
-      cands = 0;
-      bound = 0;  // (stays where fewer chunks have a key there: all keys count then)
-    }
-  }
   __syncthreads();
-  Part all = wave_part[0];
+  const RowStats r = row_stats(waves_join<kWaves>(wave_part));
+  if (tid == 0) write_row(a, row, r, token);
+  if (tid < a.top) write_top(a, row, tid, tid < found ? sel.out[tid] : 0, r);
+}
+
+// A row a block, chunk by chunk: no join, and while a block seeks its
+// alternatives the others on its unit read.
+constexpr int kRowVecs = 8, kRowGroups = 4096;  // vectors a thread and chunk; groups of a row at most
+template <class T, bool kTop>
+__global__ __launch_bounds__(kChunkThreads) void k_logp_long(LogpArgs a) {
+  constexpr int V = 16 / sizeof(T), kWaves = kChunkThreads / 64, L = kRowVecs;
+  __shared__ Part wave_part[kWaves];
+  extern __shared__ uint32_t row_groups[];  // [chunks][kGroups * L]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+  const Cut<T> cut(x, a.vocab);
+  Given token;
+  if (tid == 0) token = given(a, row, x);
+  float ex = -kInf;
+  if (tid < cut.head) ex = (float)x[tid];
+  if (tid >= V && tid < V + cut.tail) ex = (float)x[cut.head + cut.vecs * V + tid - V];
+  Part mine;
+  for (int chunk = 0; chunk < a.chunks; ++chunk) {
+    Raw p[L];
+    load_vecs<T, L>(p, x + cut.head, chunk * L * kChunkThreads + tid, kChunkThreads, cut.vecs);
+    float vm[L];
+    const Part part = thread_part<T, L>(p, chunk == 0 ? ex : -kInf, vm);
+    mine = chunk == 0 ? part : part_join(mine, part);
+    if constexpr (kTop) group_maxima<L>(vm, row_groups + chunk * (kGroups * L), tid);
+  }
+  mine = wave_join(mine);
+  if (lane == 0) wave_part[tid >> 6] = mine;
+  __syncthreads();
+  const RowStats r = row_stats(waves_join<kWaves>(wave_part));
+  if (tid == 0) write_row(a, row, r, token);
+  if constexpr (kTop) {
+    __shared__ Select<kChunkThreads> sel;
+    __shared__ uint32_t chosen[MLKV_LOGITS_MAX_TOP];
+    const int found = select_logits<T>(sel, tid, x, cut, row_groups, a.top, chosen);
+    if (tid < a.top) write_top(a, row, tid, tid < found ? sel.out[tid] : 0, r);
+  }
+}
+
+// Rows of at most 64 * L vectors: a wave each, four a block.
+template <class T, int L, bool kTop>
+__global__ __launch_bounds__(kChunkThreads) void k_logp_rows(LogpArgs a) {
+  constexpr int V = 16 / sizeof(T), kWaves = kChunkThreads / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
+  if (row >= a.n) return;
+  const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+  const Cut<T> cut(x, a.vocab);
+  Raw p[L];
+  load_vecs<T, L>(p, x + cut.head, lane, 64, cut.vecs);
+  float ex = -kInf;
+  if (lane < cut.head) ex = (float)x[lane];
+  if (lane >= V && lane < V + cut.tail) ex = (float)x[cut.head + cut.vecs * V + lane - V];
+  float vm[L];
+  Given token;
+  if (lane == 0) token = given(a, row, x);
+  const RowStats r = row_stats(wave_join(thread_part<T, L>(p, ex, vm)));
+  if (lane == 0) write_row(a, row, r, token);
+  if constexpr (kTop) {
+    __shared__ Select<64> sel[kWaves];
+    Select<64>& s = sel[wave];
+    // the lane's logits are its vectors' and perhaps one before or behind them
+    const bool has = lane < cut.head || (lane >= V && lane < V + cut.tail);
+    const uint32_t at = lane < cut.head ? lane : cut.head + cut.vecs * V + lane - V;
+    float best = has ? ex : -kInf;
+    bool any = has && ex == ex;
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) all = part_join(all, wave_part[w]);
-  const RowStats r = row_stats(all);
-  if (tid == 0) write_row<T>(a, row, r);
-  if (a.top == 0) return;
-  for (int c = tid; c < a.chunks; c += kJoinThreads) {
-    const uint64_t k = head[c];
-    if (k == 0) continue;
-    int over = 0;
-    for (int o = 0; o < a.chunks; ++o) over += head[o] > k;
-    if (over == need - 1) bound = k;
-  }
-  __syncthreads();
-  const uint64_t least = bound;
-  // `need` chunks have up to `top` keys as large as the bound, the others up to
-  // `depth`: fewer than top * (need + 1) in all. More (no bound, because NaNs
-  // left chunks without keys) only where the ids are -1 anyway.
-  const int total = a.chunks * a.top, most = a.top * (min(a.chunks, a.top) + 1);
-  for (int i = tid; i < total; i += kJoinThreads) {
-    const uint64_t k = keys[i];
-    if (k != 0 && k >= least) {
-      const int at = atomicAdd(&cands, 1);
-      if (at < most) cand[at] = k;
+    for (int j = 0; j < L; ++j) {
+      best = fmaxf(best, vm[j]);
+      any |= lane + j * 64 < cut.vecs;
     }
+    const int found = select_top<64>(s, lane, any ? value_key(best) : 0, a.top, [&](const auto& f) {
+      if (has) f(full_key(ex, at));
+#pragma unroll
+      for (int j = 0; j < L; ++j)
+        if (lane + j * 64 < cut.vecs) {
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            f(full_key(element<T>(p[j], e), (uint32_t)(cut.head + (lane + j * 64) * V + e)));
+        }
+    });
+    if (lane < a.top) write_top(a, row, lane, lane < found ? s.out[lane] : 0, r);
   }
-  __syncthreads();
-  const int nc = min(cands, most);
-  for (int i = tid; i < nc; i += kJoinThreads) {
-    const uint64_t f = cand[i];
-    int over = 0;
-    for (int o = 0; o < nc; ++o) over += cand[o] > f;
-    if (over < a.top) write_top(a, row, over, f, r);
-  }
-  for (int i = nc + tid; i < a.top; i += kJoinThreads) write_top(a, row, i, 0, r);
 }
 
 // ---- gradient ----
@@ -427,11 +628,11 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
   T* out = static_cast<T*>(a.out) + row * a.out_stride;
   const Cut<T> cut(x, a.vocab);
   const int first = chunk * kGradVecs * kChunkThreads + tid;
-  Pack<T, V> p[kGradVecs];
+  Raw p[kGradVecs] = {};
 #pragma unroll
   for (int j = 0; j < kGradVecs; ++j) {
     const int v = first + j * kChunkThreads;
-    if (v < cut.vecs) p[j] = *reinterpret_cast<const Pack<T, V>*>(x + cut.head + (int64_t)v * V);
+    if (v < cut.vecs) p[j] = load_raw(x + cut.head + (int64_t)v * V);
   }
   int extra = -1;
   if (chunk == 0 && tid < cut.head) extra = tid;
@@ -465,72 +666,90 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
       const int i = cut.head + v * V;
       LoosePack<T, V> o;
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = (T)grad_of<kEntropy>((float)p[j].v[e], i + e, g);
+      for (int e = 0; e < V; ++e) o.v[e] = (T)grad_of<kEntropy>(element<T>(p[j], e), i + e, g);
       *reinterpret_cast<LoosePack<T, V>*>(out + i) = o;
     }
   }
   if (extra >= 0) out[extra] = (T)grad_of<kEntropy>(ex, extra, g);
 }
 
-// How rows are cut: vectors a thread and chunks a row. A row that fits one
-// chunk is one, with the fewest vectors a thread; a longer one has the largest
-// chunks unless these are too few to fill the device.
-constexpr int64_t kFillBlocks = 512;
+// How rows are cut: a wave a row of few logits; a block a row, chunk by chunk,
+// where the rows fill the device; else chunks on blocks of their own and a
+// join. A row that fits one chunk is one, with the fewest vectors a thread; a
+// longer one has the largest chunks unless these are too few to fill the device.
+constexpr int64_t kFillBlocks = 512, kFillRows = 1024;
+constexpr int kWaveVecs = 128;  // vectors of a row that a wave takes
+enum Cutting : int { kWaveRow, kBlockRow, kChunks };
 struct ChunkPlan {
   int L, chunks;
+  Cutting how;
 };
 ChunkPlan chunk_plan(int64_t n, int64_t vocab, int size) {
   const int64_t vecs = vocab / (16 / size);
   ChunkPlan c;
   c.L = 1;
-  while (c.L < 8 && vecs > (int64_t)c.L * kChunkThreads) c.L *= 2;
-  const auto chunks = [&] {
-    const int64_t per = (int64_t)c.L * kChunkThreads;
-    return std::max<int64_t>(1, (vecs + per - 1) / per);
-  };
-  if (chunks() > 1)
-    while (c.L > 1 && n * chunks() < kFillBlocks) c.L /= 2;
+  c.chunks = 1;
+  c.how = vecs <= kWaveVecs ? kWaveRow : kChunks;
+  const int64_t across = c.how == kWaveRow ? 64 : kChunkThreads;
+  while (c.L < 8 && vecs > c.L * across) c.L *= 2;
+  const auto chunks = [&] { return std::max<int64_t>(1, (vecs + c.L * across - 1) / (c.L * across)); };
+  if (chunks() > 1) {
+    if (n >= kFillRows && chunks() * kGroups * kRowVecs <= kRowGroups) c.how = kBlockRow;
+    else
+      while (c.L > 1 && n * chunks() < kFillBlocks) c.L /= 2;
+  }
   c.chunks = (int)chunks();
   return c;
 }
+static_assert(kRowVecs == 8, "chunk_plan's largest chunks are those of k_logp_long");
 
 // Rows of one launch: at most 2^23 blocks (a grid has fewer than 2^32 threads).
 constexpr int64_t kGridBlocks = 1 << 23;
 
 template <class T, int L>
-hipError_t launch_chunks(const LogpArgs& a, int64_t rows, hipStream_t st) {
-  const dim3 grid((unsigned)(rows * a.chunks)), block(kChunkThreads);
-  if (a.top > 0) {
-    constexpr int V = 16 / sizeof(T);
-    hipLaunchKernelGGL((k_logp_chunk<T, L, true>), grid, block, sizeof(uint64_t) * a.top * (L * V + 1), st, a);
+hipError_t launch_chunks(const LogpArgs& a, Cutting how, hipStream_t st) {
+  const dim3 block(kChunkThreads), rows((unsigned)a.n);
+  if (how == kWaveRow) {
+    if constexpr (L <= 2) {
+      const dim3 grid((unsigned)((a.n + 3) / 4));
+      if (a.top > 0) hipLaunchKernelGGL((k_logp_rows<T, L, true>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((k_logp_rows<T, L, false>), grid, block, 0, st, a);
+    }
+  } else if (how == kBlockRow) {
+    if constexpr (L == kRowVecs) {
+      const size_t lds = sizeof(uint32_t) * a.chunks * a.chunk_groups;
+      if (a.top > 0) hipLaunchKernelGGL((k_logp_long<T, true>), rows, block, lds, st, a);
+      else hipLaunchKernelGGL((k_logp_long<T, false>), rows, block, 0, st, a);
+    }
   } else {
-    hipLaunchKernelGGL((k_logp_chunk<T, L, false>), grid, block, 0, st, a);
+    const dim3 grid((unsigned)(a.n * a.chunks));
+    if (a.top == 0) hipLaunchKernelGGL((k_logp_chunk<T, L, kNoTop>), grid, block, 0, st, a);
+    else if (a.chunks > 1) hipLaunchKernelGGL((k_logp_chunk<T, L, kLeaveTop>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_logp_chunk<T, L, kTakeTop>), grid, block, 0, st, a);
+    if (a.chunks > 1) hipLaunchKernelGGL((k_logp_join<T>), rows, block, 0, st, a);
   }
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t launch_logp(LogpArgs a, int L, hipStream_t st) {
+hipError_t launch_logp(LogpArgs a, const ChunkPlan& c, hipStream_t st) {
   const int64_t slice = std::max<int64_t>(1, kGridBlocks / a.chunks), n = a.n;
   for (int64_t at = 0; at < n; at += slice) {
-    const int64_t rows = std::min(slice, n - at);
-    hipError_t e = L == 1 ? launch_chunks<T, 1>(a, rows, st) : L == 2 ? launch_chunks<T, 2>(a, rows, st)
-                 : L == 4 ? launch_chunks<T, 4>(a, rows, st) : launch_chunks<T, 8>(a, rows, st);
-    if (e == hipSuccess && a.chunks > 1) {
-      hipLaunchKernelGGL((k_logp_join<T>), dim3((unsigned)rows), dim3(kJoinThreads),
-                         a.top ? join_lds(a.chunks, a.top) : 0, st, a);
-      e = hipGetLastError();
-    }
+    a.n = std::min(slice, n - at);
+    const hipError_t e = c.L == 1 ? launch_chunks<T, 1>(a, c.how, st) : c.L == 2 ? launch_chunks<T, 2>(a, c.how, st)
+                       : c.L == 4 ? launch_chunks<T, 4>(a, c.how, st) : launch_chunks<T, 8>(a, c.how, st);
     if (e != hipSuccess) return e;
-    a.logits = static_cast<const T*>(a.logits) + rows * a.stride;
-    if (a.tokens != nullptr) a.tokens += rows;
-    if (a.logp != nullptr) a.logp += rows;
-    if (a.entropy != nullptr) a.entropy += rows;
-    if (a.stats != nullptr) a.stats += 2 * rows;
-    if (a.top_ids != nullptr) a.top_ids += rows * a.top;
-    if (a.top_logp != nullptr) a.top_logp += rows * a.top;
-    a.parts += rows * a.chunks;
-    a.keys += rows * a.chunks * a.top;
+    a.logits = static_cast<const T*>(a.logits) + a.n * a.stride;
+    if (a.tokens != nullptr) a.tokens += a.n;
+    if (a.logp != nullptr) a.logp += a.n;
+    if (a.entropy != nullptr) a.entropy += a.n;
+    if (a.stats != nullptr) a.stats += 2 * a.n;
+    if (a.top_ids != nullptr) a.top_ids += a.n * a.top;
+    if (a.top_logp != nullptr) a.top_logp += a.n * a.top;
+    if (a.parts != nullptr) {
+      a.parts += a.n * a.chunks;
+      a.groups += a.n * a.chunks * a.chunk_groups;
+    }
   }
   return hipSuccess;
 }
@@ -582,8 +801,8 @@ int64_t mlkv_log_probs_workspace(int64_t n, int64_t vocab, int32_t top, int dtyp
   if (top < 0 || top > MLKV_LOGITS_MAX_TOP || top > vocab)
     return op_error(MLKV_EINVAL, "top must be in [0, min(vocab, 64)]");
   const ChunkPlan c = chunk_plan(n, vocab, dtype_size(dtype));
-  if (c.chunks == 1) return 0;
-  return n * c.chunks * (int64_t)(sizeof(Part) + sizeof(uint64_t) * top);
+  if (c.how != kChunks || c.chunks == 1) return 0;
+  return n * c.chunks * (int64_t)(sizeof(Part) + (top > 0 ? sizeof(uint32_t) * kGroups * c.L : 0));
 }
 
 int mlkv_log_probs(const void* d_logits, int64_t stride, const int64_t* d_tokens, int64_t n, int64_t vocab,
@@ -614,15 +833,18 @@ int mlkv_log_probs(const void* d_logits, int64_t stride, const int64_t* d_tokens
   a.stats = d_stats;
   a.top_ids = d_top_ids;
   a.top_logp = d_top_logp;
-  a.parts = static_cast<Part*>(d_work);
-  a.keys = reinterpret_cast<uint64_t*>(static_cast<char*>(d_work) + sizeof(Part) * (size_t)(n * c.chunks));
+  if (bytes > 0) {
+    a.parts = static_cast<Part*>(d_work);
+    a.groups = reinterpret_cast<uint32_t*>(static_cast<char*>(d_work) + sizeof(Part) * (size_t)(n * c.chunks));
+  }
   a.stride = stride;
   a.n = n;
   a.vocab = (int)vocab;
   a.top = d_top_ids != nullptr || d_top_logp != nullptr ? top : 0;
   a.chunks = c.chunks;
+  a.chunk_groups = kGroups * c.L;
   const hipError_t e = dispatch_type(dtype, [&](auto t) {
-    return launch_logp<decltype(t)>(a, c.L, static_cast<hipStream_t>(hip_stream));
+    return launch_logp<decltype(t)>(a, c, static_cast<hipStream_t>(hip_stream));
   });
   return e == hipSuccess ? MLKV_OK : op_launch_error(e, "mlkv_log_probs launch");
 }

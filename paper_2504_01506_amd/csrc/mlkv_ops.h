@@ -49,13 +49,8 @@ inline bool stride_ok(int64_t stride, int64_t rows, int64_t width, bool same) {
   return stride >= width && stride <= (int64_t(1) << 60) / rows;
 }
 
-// V elements of T as one load or store, at a multiple of its size ...
-template <class T, int V>
-struct __align__(sizeof(T) * V) Pack {
-  T v[V];
-};
-// ... or at any address that T may have: the same 16-byte instruction, which
-// the memory pipeline takes at any alignment.
+// V elements of T as one load or store at any address that T may have: 16
+// bytes are one instruction, which the memory pipeline takes at any alignment.
 template <class T, int V>
 struct __attribute__((packed, aligned(sizeof(T)))) LoosePack {
   T v[V];
@@ -87,8 +82,12 @@ __device__ __forceinline__ float element(const Raw& r, int j) {
 // data-parallel moves (xor 1, xor 2, then mirrors, which meet equal values),
 // then by exchanging rows of 16 and halves of the wave.
 template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_bits(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xF, 0xF, false);
+}
+template <int kCtrl>
 __device__ __forceinline__ float dpp_move(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, false));
+  return __uint_as_float(dpp_bits<kCtrl>(__float_as_uint(v)));
 }
 __device__ __forceinline__ float group_sum(float v, int G) {
   if (G > 1) v += dpp_move<0xB1>(v);    // quad_perm 1 0 3 2
@@ -104,6 +103,18 @@ __device__ __forceinline__ float group_sum(float v, int G) {
     v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
   }
   return v;
+}
+
+// The largest v of a wave, in every lane (a NaN counts only beside NaNs).
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp_move<0xB1>(v));
+  v = fmaxf(v, dpp_move<0x4E>(v));
+  v = fmaxf(v, dpp_move<0x141>(v));
+  v = fmaxf(v, dpp_move<0x140>(v));
+  auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 
 }  // namespace mlkv

@@ -42,7 +42,7 @@ def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=Non
         raise ValueError(f"{what} is on {t.device}, not on {like.device}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")

@@ -95,7 +95,18 @@ def test_vocabularies(gen, vocab, kind):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,vocab,top", [(2000, 300, 3), (700, 33_000, 10), (129, 20_000, 64), (3, 600_000, 50),
+@pytest.mark.parametrize("vocab", [40, 900, 6000, 40_000])
+@pytest.mark.parametrize("far", [300.0, -3e4, 6e4, 1e8, -1e30, 3e37, 2e38])
+def test_far_logits(gen, vocab, far):
+    # a row's own offset is no part of its distribution, as far as its digits go
+    for kind in (torch.float32, torch.bfloat16):
+        x = logits(gen, 5, vocab, torch.float32)
+        x = (far + x * max(1.0, abs(far) * 2.0 ** -20)).to(kind)
+        check(x, some_tokens(gen, 5, vocab), 9)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vocab,top", [(2000, 300, 3), (700, 33_000, 10), (129, 20_000, 64), (3, 600_000, 50), (1100, 20_000, 10), (1025, 5001, 64),
                                          (1, 2_000_001, 64), (40, 262_144, 33)])
 def test_many_rows_and_long_rows(gen, n, vocab, top):
     for kind in (torch.float32, torch.bfloat16):
@@ -113,9 +124,29 @@ def test_ties(gen, vocab, kind):
     x[3, ::2] = -0.0                                        # zeros of both signs are equal
     x[4] = torch.arange(vocab, device="cuda").to(kind) * 1e-3   # rising: the largest last
     x[5] = -x[4]
+    y = x.clone()
+    y[:, vocab // 2:vocab // 2 + 5] = 4.0
+    check(y, t, min(64, vocab))
     for top in (1, 17, 64):
         check(x, t, top)
         check(x[:, 1:], t.clamp(max=vocab - 2), top)        # rows off their 16-byte boundaries
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [3000, 40_000])
+def test_ties_and_masks_in_many_rows(gen, vocab, kind):
+    # rows enough for each to be a block's
+    x = torch.zeros((8, vocab), dtype=kind, device="cuda")
+    x[1] = torch.randint(3, (vocab,), generator=gen, device="cuda").to(kind)
+    x[2] = torch.arange(vocab, device="cuda").to(kind) * 1e-3
+    x[3], x[3, 77:90] = -math.inf, 1.0
+    x[4] = -math.inf
+    x[5], x[5, ::50] = torch.finfo(kind).min, 2.0
+    x[6:] = logits(gen, 2, vocab, kind)
+    x, t = x.repeat(160, 1), some_tokens(gen, 1280, vocab)
+    for top in (1, 20, 64):
+        check(x, t, top)
 
 
 @pytest.mark.gpu
@@ -333,7 +364,7 @@ def test_gradient_refusals(change, says):
 def test_workspace_sizes():
     size = mlkv.mlkv_log_probs_workspace
     assert size(5, 64, 4, mlkv.MLKV_F32) == 0 and size(0, 10 ** 6, 4, mlkv.MLKV_F32) == 0
-    assert size(4096, 128_000, 5, mlkv.MLKV_BF16) > 0
+    assert size(40, 128_000, 5, mlkv.MLKV_BF16) > 0
     for bad in ((-1, 64, 4, 0), (1, 0, 0, 0), (1, 64, 65, 0), (1, 64, 4, 5), (1, 2 ** 24 + 1, 1, 0)):
         assert size(*bad) == mlkv.MLKV_EINVAL
 
