@@ -174,9 +174,9 @@ struct Cut {
 };
 
 // ---- the k largest keys of a team (a wave or a block) ----
-// The k-th largest of the threads' (of a block: of every four threads') largest
-// values, cut to 16 bits, is a bound that the k largest reach; the keys over
-// it, hardly more than k, are ranked by counting. Many equal values can leave
+// The k-th largest of the threads' largest values, cut to 16 bits, is a bound
+// that the k largest reach; the keys over it, hardly more than k, are ranked by
+// counting. Many equal values can leave
 // more than kCands of them: then the bound is the k-th largest of the threads'
 // own largest keys, which no more than k threads reach, and where even those
 // hold too many (large ones in few threads), the largest key below the last is
@@ -184,7 +184,7 @@ struct Cut {
 template <int kTeam>
 struct Select {
   static constexpr int kCands = kTeam == 64 ? 512 : 1024;
-  uint32_t quad[64];
+  uint32_t seen[kTeam];
   uint64_t list[kTeam];
   uint64_t cand[kCands];
   uint64_t out[MLKV_LOGITS_MAX_TOP];  // largest first
@@ -220,19 +220,31 @@ template <int kTeam, class Each>
 __device__ __forceinline__ int select_top(Select<kTeam>& s, int tid, uint32_t q, int k, const Each& each) {
   constexpr int kCands = Select<kTeam>::kCands;
   const int lane = tid & 63;
-  if constexpr (kTeam > 64) {
-    uint32_t t = max(q, dpp_bits<0xB1>(q));
-    t = max(t, dpp_bits<0x4E>(t));
-    if ((lane & 3) == 0) s.quad[tid >> 2] = t;
-  }
+  s.seen[tid] = q;
   if (tid == 0) s.listed = s.cands = 0;
   team_sync<kTeam>();
-  const uint32_t seen = kTeam > 64 ? s.quad[lane] : q;
-  uint32_t low = 0;
+  uint32_t seen[kTeam / 64], most = 0, low = 0;
+#pragma unroll
+  for (int w = 0; w < kTeam / 64; ++w) {
+    seen[w] = s.seen[w * 64 + lane];
+    most = max(most, seen[w]);
+  }
+  // (few keys: the largest of every four threads will do, a quarter of the work)
+  if (kTeam == 64 || k <= 16) {
 #pragma unroll 1
-  for (int bit = 31; bit >= 16; --bit) {
-    const uint32_t t = low | 1u << bit;
-    if (__popcll(__ballot(seen >= t)) >= k) low = t;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t t = low | 1u << bit;
+      if (__popcll(__ballot(most >= t)) >= k) low = t;
+    }
+  } else {
+#pragma unroll 1
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t t = low | 1u << bit;
+      int reach = 0;
+#pragma unroll
+      for (int w = 0; w < kTeam / 64; ++w) reach += __popcll(__ballot(seen[w] >= t));
+      if (reach >= k) low = t;
+    }
   }
   const auto collect = [&](uint64_t least) {
     each([&](uint64_t f) {
@@ -327,20 +339,43 @@ static_assert(kChunkThreads == 256, "select_top's slow way joins four waves");
 template <class T>
 __device__ __forceinline__ int select_logits(Select<kChunkThreads>& s, int tid, const T* x, const Cut<T>& cut,
                                              const uint32_t* groups, int k, uint32_t* chosen) {
-  constexpr int V = 16 / sizeof(T), kSize = kGroupVecs * V;
+  constexpr int V = 16 / sizeof(T);
   const int ng = (cut.vecs + kGroupVecs - 1) / kGroupVecs;
   const int nsel = select_of<kChunkThreads>(s, tid, ng, k, [&](int i) { return (uint64_t)groups[i] << 32 | (uint32_t)~i; });
   if (tid < nsel) chosen[tid] = key_index(s.out[tid]);
   __syncthreads();
-  // their logits, and those before and behind the vectors
-  const int inside = nsel * kSize, all = inside + cut.head + cut.tail, end = cut.head + cut.vecs * V;
-  return select_of<kChunkThreads>(s, tid, all, k, [&](int i) {
-    const int in = i < inside ? cut.head + (int)chosen[i / kSize] * kSize + i % kSize : end;
-    const int beside = i - inside < cut.head ? i - inside : end + (i - inside - cut.head);
-    const bool is = i >= inside || in < end;  // (the row's last group may be short)
-    const int at = i >= inside ? beside : min(in, end - 1);
-    const uint64_t f = full_key((float)x[at], (uint32_t)at);
-    return is ? f : 0;
+  // their vectors, and the logits before and behind all vectors, one a thread
+  constexpr int kMost = MLKV_LOGITS_MAX_TOP * kGroupVecs / kChunkThreads;
+  Raw p[kMost];
+  int at[kMost];
+#pragma unroll
+  for (int j = 0; j < kMost; ++j) {
+    const int i = tid + j * kChunkThreads;
+    const int v = i < nsel * kGroupVecs ? (int)chosen[i / kGroupVecs] * kGroupVecs + i % kGroupVecs : cut.vecs;
+    at[j] = v < cut.vecs ? cut.head + v * V : -1;
+    if (v < cut.vecs) p[j] = load_raw(x + at[j]);
+  }
+  int extra = -1;
+  if (tid < cut.head) extra = tid;
+  if (tid >= V && tid < V + cut.tail) extra = cut.head + cut.vecs * V + tid - V;
+  const uint64_t ex = extra >= 0 ? full_key((float)x[extra], (uint32_t)extra) : 0;
+  uint32_t q = (uint32_t)(ex >> 32);
+#pragma unroll
+  for (int j = 0; j < kMost; ++j)
+    if (at[j] >= 0) {
+      float m = -kInf;
+#pragma unroll
+      for (int e = 0; e < V; ++e) m = fmaxf(m, element<T>(p[j], e));
+      q = max(q, value_key(m));
+    }
+  return select_top<kChunkThreads>(s, tid, q, k, [&](const auto& f) {
+    f(ex);
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+      if (at[j] >= 0) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f(full_key(element<T>(p[j], e), (uint32_t)(at[j] + e)));
+      }
   });
 }
 
