@@ -12,9 +12,17 @@
 // and lo in its range. A product takes hi hi + hi lo + lo hi; what is left out
 // is 2^-22 of it, below the rounding of the fp32 sums. Bound by the matrix
 // units: three fp16 products instead of one fp32 product, at 16 times the rate.
+//
+// For an update in bf16, 8 bits, the products take hi alone and A and B have no
+// lo: 11 bits of each operand, while X is carried on as a pair (with X in 11
+// bits a step's rounding would grow in the directions of small singular
+// values). The result is then off by 0.5 to 1.3e-3 of its norm, under bf16's
+// own 1.7e-3, at a third of the products. Matrices of at most kSmall rows,
+// where it is up to 1.8e-3 and products cost little, take the pairs.
 #include "mlkv_ops.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace mlkv {
@@ -23,7 +31,8 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kThreads = 256;
 constexpr int kDepth = 32;       // k of a stage: 64 bytes a row and plane
-constexpr int kNormBlocks = 64;  // sums of squares a matrix
+constexpr int kNormBlocks = 512; // sums of squares a matrix, at most
+constexpr int kSmall = 128;
 
 using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
@@ -41,21 +50,52 @@ struct User {
   int64_t g_batch, g_row, o_batch, o_row;
 };
 
+// Lets a kernel take more LDS than 64 KB on the current device, once a device.
+template <auto kKernel>
+hipError_t allow_lds(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 // ---- norm and first X ----
+// A wave a row in turn.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_norm(User u, int64_t rows, int64_t cols, double* sums) {
+  constexpr int V = 16 / sizeof(T), kUnroll = 4;
   __shared__ double part[kThreads / 64];
   const T* g = static_cast<const T*>(u.g) + blockIdx.y * u.g_batch;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int vecs = (int)(cols / V);
   double t = 0.0;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int64_t c = threadIdx.x; c < cols; c += kThreads) {
-      const double v = (double)(float)g[r * u.g_row + c];
-      t += v * v;
+  const auto add = [&](float x) { t = __builtin_fma((double)x, (double)x, t); };
+  for (int64_t r = blockIdx.x * 4 + wave; r < rows; r += gridDim.x * 4) {
+    const T* row = g + r * u.g_row;
+    for (int v = lane; v < vecs; v += 64 * kUnroll) {
+      Raw p[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        p[k] = Raw{0, 0, 0, 0};
+        if (v + 64 * k < vecs) p[k] = load_raw(row + (int64_t)(v + 64 * k) * V);
+      }
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) add(element<T>(p[k], e));
     }
+    const int rest = vecs * V + lane;
+    if (rest < cols) add((float)row[rest]);
+  }
   for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+  if (lane == 0) part[wave] = t;
   __syncthreads();
-  if (threadIdx.x == 0) sums[blockIdx.y * kNormBlocks + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+  if (threadIdx.x == 0) sums[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
@@ -75,8 +115,13 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const double* sums, int nsums, float eps,
                                                          Planes straight, Planes turned, int rows, int cols) {
   __shared__ float tile[64][65];
+  __shared__ double part[kThreads / 64];
   double t = 0.0;
-  for (int k = 0; k < nsums; ++k) t += sums[blockIdx.z * kNormBlocks + k];
+  for (int k = threadIdx.x; k < nsums; k += kThreads) t += sums[(int64_t)blockIdx.z * nsums + k];
+  for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+  __syncthreads();
+  t = part[0] + part[1] + part[2] + part[3];
   const double inv = 32768.0 / (sqrt(t) + (double)eps);
   const T* g = static_cast<const T*>(u.g) + blockIdx.z * u.g_batch;
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
@@ -124,14 +169,23 @@ using global_ptr = const __attribute__((address_space(1))) void*;
 // lanes that LDS serves at a time then read 8 different bank groups.
 __device__ __forceinline__ int piece(int r, int c) { return r * kDepth + ((c ^ (r >> 1)) & 3) * 8; }
 
+// Waits until at most kLater of the wave's loads are in flight, then for the
+// block's other waves.
+template <int kLater>
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLater) : "memory");
+}
+
 // A tile of kTile x kTile by four waves, a quarter each, in blocks of 32 x 32.
-// Two stages of kDepth in LDS, one being filled from memory while the other is
-// multiplied.
-template <class T, int kTile, int kStep>
+// kStages stages of kDepth in LDS: while one is multiplied, the others are on
+// their way from memory. 64 KB, so that two blocks run on a unit.
+template <class T, int kTile, int kPlanes, int kStep>
 __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
-  constexpr int kPlanes = 2, kBlocks = kTile / 64;
+  constexpr int kBlocks = kTile / 64;
   constexpr int kStage = 2 * kPlanes * kTile * kDepth;  // halves
-  __shared__ __align__(16) _Float16 lds[2 * kStage];
+  constexpr int kStages = 65536 / (int)(kStage * sizeof(_Float16));
+  constexpr int kLoads = 2 * kPlanes * kTile / 16 / 4;  // of a wave and stage
+  __shared__ __align__(16) _Float16 lds[kStages * kStage];
   constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // neighbouring tiles on one XCD (blocks go round the 8 in turn), for its L2
@@ -154,17 +208,20 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
   const _Float16* Q = a.Q.p + blockIdx.z * a.Q.batch + (int64_t)bj * kTile * a.Q.ld;
 
   // 16 rows of a plane a load: lane l fetches piece (l & 3) ^ ... of row l / 4
-  const auto fill = [&](int stage, int k0) {
-    constexpr int kLoads = 2 * kPlanes * kTile / 16;
+  const _Float16* from[kLoads];
 #pragma unroll
-    for (int q = 0; q < kLoads / 4; ++q) {
-      const int seg = q * 4 + wave;
-      const int plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
-      const Planes& o = plane < kPlanes ? a.P : a.Q;
-      const _Float16* from = (plane < kPlanes ? P : Q) + (plane % kPlanes) * o.plane;
-      from += (int64_t)(rows + lane / 4) * o.ld + k0 + (((lane & 3) ^ (lane >> 3)) & 3) * 8;
-      _Float16* to = lds + stage * kStage + plane * kTile * kDepth + rows * kDepth;
-      __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)to, 16, 0, 0);
+  for (int q = 0; q < kLoads; ++q) {
+    const int seg = q * 4 + wave, plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
+    const Planes& o = plane < kPlanes ? a.P : a.Q;
+    from[q] = (plane < kPlanes ? P : Q) + (plane % kPlanes) * o.plane + (int64_t)(rows + lane / 4) * o.ld +
+              (((lane & 3) ^ (lane >> 3)) & 3) * 8;
+  }
+  const auto fill = [&](int t) {
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) {
+      const int seg = q * 4 + wave, plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
+      _Float16* to = lds + (t % kStages) * kStage + plane * kTile * kDepth + rows * kDepth;
+      __builtin_amdgcn_global_load_lds((global_ptr)(from[q] + t * kDepth), (lds_ptr)to, 16, 0, 0);
     }
   };
 
@@ -178,12 +235,15 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
 
   const int wi = (wave >> 1) * (kTile / 2), wj = (wave & 1) * (kTile / 2);
   const int stages = a.k / kDepth;
-  fill(0, 0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < kStages - 1; ++t)
+    if (t < stages) fill(t);
   for (int t = 0; t < stages; ++t) {
-    if (t + 1 < stages) fill((t + 1) & 1, (t + 1) * kDepth);
-    const _Float16* st = lds + (t & 1) * kStage;
+    // stage t is there, and all waves are done with stage t - 1, whose place is filled next
+    if (t + kStages - 2 < stages) stage_barrier<(kStages - 2) * kLoads>();
+    else stage_barrier<0>();
+    if (t + kStages - 1 < stages) fill(t + kStages - 1);
+    const _Float16* st = lds + (t % kStages) * kStage;
 #pragma unroll
     for (int h = 0; h < kDepth / 16; ++h) {
       half8 p[kBlocks][kPlanes], q[kBlocks][kPlanes];
@@ -201,15 +261,16 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
 #pragma unroll
         for (int y = 0; y < kBlocks; ++y) {
           acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][0], acc[x][y], 0, 0, 0);
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][1], acc[x][y], 0, 0, 0);
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][1], q[y][0], acc[x][y], 0, 0, 0);
+          if constexpr (kPlanes == 2) {
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][1], acc[x][y], 0, 0, 0);
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][1], q[y][0], acc[x][y], 0, 0, 0);
+          }
         }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
   }
 
   // Epilogue. A lane holds column j = lane % 32 of each block, rows i in fours.
+  constexpr bool kPairIn = kPlanes == 2 || !kSym, kPairOut = kPlanes == 2 || kStep == kApplyB;
   const _Float16* add = kStep == kSquareX ? nullptr : a.add.p + blockIdx.z * a.add.batch;
   _Float16* out = kStep == kApplyLast ? nullptr : a.out.p + blockIdx.z * a.out.batch;
 #pragma unroll
@@ -227,7 +288,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
         } else {
           const int64_t at = (int64_t)j * a.add.ld + i;
           const half4 hi = *reinterpret_cast<const half4*>(add + at);
-          const half4 lo = *reinterpret_cast<const half4*>(add + a.add.plane + at);
+          half4 lo = {};
+          if constexpr (kPairIn) lo = *reinterpret_cast<const half4*>(add + a.add.plane + at);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float old = (float)hi[e] + (float)lo[e];
@@ -254,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
           }
           const int64_t at = (int64_t)j * a.out.ld + i;
           *reinterpret_cast<half4*>(out + at) = hi;
-          *reinterpret_cast<half4*>(out + a.out.plane + at) = lo;
+          if constexpr (kPairOut) *reinterpret_cast<half4*>(out + a.out.plane + at) = lo;
           if (kStep == kApplyB || (kSym && bi != bj)) {
             const Planes& o = kSym ? a.out : a.out2;
             _Float16* to = o.p + blockIdx.z * o.batch;
@@ -262,11 +324,201 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
             for (int e = 0; e < 4; ++e) {
               const int64_t to_at = (int64_t)(i + e) * o.ld + j;
               to[to_at] = hi[e];
-              to[o.plane + to_at] = lo[e];
+              if constexpr (kPlanes == 2) to[o.plane + to_at] = lo[e];  // (of X only the products read this one)
             }
           }
         }
       }
+}
+
+// ---- small matrices: all steps in one block ----
+// Matrices of at most 64 x 256 (as iterated on) live in LDS, X and X^T as
+// pairs, A, and B in the place of X X^T's second half sums: all 160 KB of a
+// unit. Eight waves: X X^T a block of 32 x 32 and half the sum each, A A the
+// blocks, B X 32 columns each. Bound by the latency of its chain: three products
+// and four exchanges through LDS a step.
+constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
+constexpr int kTinyX = kTinyM * kTinyN, kTinyA = kTinyM * kTinyM;  // halves of a plane
+constexpr size_t kTinyLds = sizeof(_Float16) * (4 * kTinyX + 4 * kTinyA);
+
+// Element k of row r of a plane with rows of kRow halves. Pieces of 16 bytes are
+// exchanged by the row, so that 8 lanes that read a column of pieces meet 8
+// different bank groups.
+template <int kRow>
+__device__ __forceinline__ int spot(int r, int k) { return r * kRow + (((k >> 3) ^ (r & 7)) << 3) + (k & 7); }
+
+template <class T>
+__global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, int cols, bool turned, int steps,
+                                                            float eps) {
+  extern __shared__ __align__(16) _Float16 lds_tiny[];
+  _Float16* X = lds_tiny;                // [2][64][256]
+  _Float16* XT = X + 2 * kTinyX;         // [2][256][64]
+  _Float16* A = XT + 2 * kTinyX;         // [2][64][64]
+  _Float16* B = A + 2 * kTinyA;          // [2][64][64]
+  float4* half = reinterpret_cast<float4*>(B);  // [4 blocks][4][64 lanes]: the sums' second halves, before B
+  double* part = reinterpret_cast<double*>(A);  // [8], before A
+  int lane = threadIdx.x & 63;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const T* g = static_cast<const T*>(u.g) + blockIdx.x * u.g_batch;
+  const int m = turned ? cols : rows, n = turned ? rows : cols;
+
+  // G's rows along the threads: 64 x 256, or 256 x 64 where it is turned
+  constexpr int kEach = kTinyX / kTinyThreads;
+  const int wide = turned ? 6 : 8;  // log2 of that
+  float v[kEach];
+  double t = 0.0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int at = e * kTinyThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
+    v[e] = r < rows && c < cols ? (float)g[r * u.g_row + c] : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) t = __builtin_fma((double)v[e], (double)v[e], t);
+  for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+  if (lane == 0) part[wave] = t;
+  __syncthreads();
+  t = 0.0;
+  for (int w = 0; w < kTinyThreads / 64; ++w) t += part[w];
+  const double inv = 32768.0 / (sqrt(t) + (double)eps);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int at = e * kTinyThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
+    const int i = turned ? c : r, j = turned ? r : c;
+    _Float16 hi, lo;
+    split((float)((double)v[e] * inv), hi, lo);
+    X[spot<kTinyN>(i, j)] = hi;
+    X[kTinyX + spot<kTinyN>(i, j)] = lo;
+    XT[spot<kTinyM>(j, i)] = hi;
+    XT[kTinyX + spot<kTinyM>(j, i)] = lo;
+  }
+  __syncthreads();
+
+  const int bi = (wave >> 1) & 1, bj = wave & 1, second = wave >> 2;  // of X X^T and A A
+  // sums over pieces of 16 of k, from k0 on, of the block of rows p0 and q0 of planes of rows of kRow
+  const auto multiply = [&](auto width, const _Float16* P, int p0, const _Float16* Q, int q0, int plane_p,
+                            int plane_q, int k0, int count) {
+    constexpr int kRow = decltype(width)::value;
+    float16v a, b, c;  // (three chains of dependent products)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) a[e] = b[e] = c[e] = 0.0f;
+    const int row = lane & 31, deep = (lane >> 5) * 8;
+    // two pieces at a time; one too many is of zeros
+    for (int t = 0; t < count; t += 2) {
+      half8 ph[2], pl[2], qh[2], ql[2];
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int k = k0 + (t + d) * 16;
+        const int sp = spot<kRow>(p0 + row, k + deep), sq = spot<kRow>(q0 + row, k + deep);
+        ph[d] = *reinterpret_cast<const half8*>(P + sp);
+        pl[d] = *reinterpret_cast<const half8*>(P + plane_p + sp);
+        qh[d] = *reinterpret_cast<const half8*>(Q + sq);
+        ql[d] = *reinterpret_cast<const half8*>(Q + plane_q + sq);
+      }
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        a = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[d], qh[d], a, 0, 0, 0);
+        b = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[d], ql[d], b, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[d], qh[d], c, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) a[e] += b[e] + c[e];
+    return a;
+  };
+  // calls f(i, j, e): elements e .. e + 3 of a block at (i0, j0) are those at (i .. i + 3, j)
+  const auto fours = [&](int i0, int j0, const auto& f) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) f(i0 + e * 2 + (lane >> 5) * 4, j0 + (lane & 31), e);
+  };
+  const auto halves = [](const float16v& x, int e, half4& hi, half4& lo) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      _Float16 h, l;
+      split(x[e + d], h, l);
+      hi[d] = h;
+      lo[d] = l;
+    }
+  };
+  // (A and B are symmetric: written as [j][i])
+  const auto put = [&](_Float16* to, const float16v& x) {
+    fours(bi * 32, bj * 32, [&](int i, int j, int e) {
+      half4 hi, lo;
+      halves(x, e, hi, lo);
+      *reinterpret_cast<half4*>(to + spot<kTinyM>(j, i)) = hi;
+      *reinterpret_cast<half4*>(to + kTinyA + spot<kTinyM>(j, i)) = lo;
+    });
+  };
+  using OfX = std::integral_constant<int, kTinyN>;
+  using OfA = std::integral_constant<int, kTinyM>;
+  // pieces of the sum over n: an even number for each half, those behind n of zeros
+  const int each = ((n + 15) / 16 + 3) / 4 * 2;
+  for (int step = 0; step < steps; ++step) {
+    asm volatile("" : "+v"(lane));  // (places in LDS are worked out again: kept over the steps they take all registers)
+    float16v s = multiply(OfX{}, X, bi * 32, X, bj * 32, kTinyX, kTinyX, second ? each * 16 : 0, each);
+    if (second) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        half[((wave & 3) * 4 + e / 4) * 64 + lane] = make_float4(s[e], s[e + 1], s[e + 2], s[e + 3]);
+    }
+    __syncthreads();
+    if (!second) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const float4 h = half[(wave * 4 + e / 4) * 64 + lane];
+        s[e] = (s[e] + h.x) * 0x1p-15f;
+        s[e + 1] = (s[e + 1] + h.y) * 0x1p-15f;
+        s[e + 2] = (s[e + 2] + h.z) * 0x1p-15f;
+        s[e + 3] = (s[e + 3] + h.w) * 0x1p-15f;
+      }
+      put(A, s);
+    }
+    __syncthreads();
+    if (!second) {
+      const float16v q = multiply(OfA{}, A, bi * 32, A, bj * 32, kTinyA, kTinyA, 0, 4);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(kC * 0x1p-16f, q[e], kB * 0.5f * s[e]);
+      put(B, s);
+    }
+    __syncthreads();
+    // the wave's 32 columns; no other wave reads their rows of X^T, and none X
+    const int j0 = wave * 32;
+    if (j0 < n) {
+      float16v y[2];  // both are computed before either is written
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        y[x] = multiply(OfA{}, B, x * 32, XT, j0, kTinyA, kTinyX, 0, 4);
+        fours(x * 32, j0, [&](int i, int j, int e) {
+          const half4 hi = *reinterpret_cast<const half4*>(XT + spot<kTinyM>(j, i));
+          const half4 lo = *reinterpret_cast<const half4*>(XT + kTinyX + spot<kTinyM>(j, i));
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            y[x][e + d] = __builtin_fmaf(0x1p-14f, y[x][e + d], kA * ((float)hi[d] + (float)lo[d]));
+        });
+      }
+      T* out = static_cast<T*>(u.out) + blockIdx.x * u.o_batch;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        fours(x * 32, j0, [&](int i, int j, int e) {
+          if (step + 1 < steps) {
+            half4 hi, lo;
+            halves(y[x], e, hi, lo);
+            *reinterpret_cast<half4*>(XT + spot<kTinyM>(j, i)) = hi;
+            *reinterpret_cast<half4*>(XT + kTinyX + spot<kTinyM>(j, i)) = lo;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              X[spot<kTinyN>(i + d, j)] = hi[d];
+              X[kTinyX + spot<kTinyN>(i + d, j)] = lo[d];
+            }
+          } else if (j < n) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+              if (i + d < m)
+                out[turned ? j * u.o_row + i + d : (i + d) * u.o_row + j] = (T)(y[x][e + d] * 0x1p-15f);
+          }
+        });
+    }
+    __syncthreads();
+  }
 }
 
 struct Layout {
@@ -274,6 +526,8 @@ struct Layout {
   int tile;
   int64_t xs, as;  // elements of a plane of X and of A
   int64_t sums, bytes;  // offset of the sums of squares; all
+  int nsums;            // of a matrix
+  bool tiny;            // one block a matrix, no workspace
 };
 
 // Tiles of 128 unless they are fewer than the device's units.
@@ -284,6 +538,11 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   l.s.n = (int)std::max(rows, cols);
   const auto up = [](int64_t v, int64_t t) { return (v + t - 1) / t * t; };
   const int64_t t128 = up(l.s.m, 128) / 128;
+  l.tiny = l.s.m <= kTinyM && l.s.n <= kTinyN;
+  if (l.tiny) {
+    l.bytes = 0;
+    return l;
+  }
   l.tile = batch * t128 * (t128 + 1) / 2 >= 256 ? 128 : 64;
   l.s.mp = (int)up(l.s.m, l.tile);
   l.s.np = (int)up(l.s.n, l.tile);
@@ -292,19 +551,21 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   // X, two of X^T, A and B, two planes each
   l.sums = batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16);
   l.sums = up(l.sums, 256);
-  l.bytes = l.sums + batch * kNormBlocks * (int64_t)sizeof(double);
+  l.nsums = (int)std::min<int64_t>((rows + 3) / 4, kNormBlocks);
+  // (as many bytes for a matrix as for its transpose)
+  l.bytes = l.sums + batch * std::min<int64_t>((l.s.n + 3) / 4, kNormBlocks) * (int64_t)sizeof(double);
   return l;
 }
 
-template <class T, int kTile, int kStep>
+template <class T, int kTile, int kPlanes, int kStep>
 hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
   constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
   const unsigned tiles = kSym ? (unsigned)(a.ti * (a.ti + 1) / 2) : (unsigned)(a.ti * a.tj);
-  hipLaunchKernelGGL((k_orth_product<T, kTile, kStep>), dim3(tiles, 1, (unsigned)batch), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((k_orth_product<T, kTile, kPlanes, kStep>), dim3(tiles, 1, (unsigned)batch), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 
-template <class T, int kTile>
+template <class T, int kTile, int kPlanes>
 hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, char* work, hipStream_t st, Planes X,
                    Planes XT0, Planes XT1, Planes A, Planes B) {
   Planes now = XT0, next = XT1;
@@ -317,18 +578,18 @@ hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, cha
     a.P = a.Q = X;
     a.out = A;
     a.k = l.s.np;
-    hipError_t e = product<float, kTile, kSquareX>(a, batch, st);
+    hipError_t e = product<float, kTile, kPlanes, kSquareX>(a, batch, st);
     if (e != hipSuccess) return e;
     a.P = a.Q = a.add = A;
     a.out = B;
     a.k = l.s.mp;
-    if ((e = product<float, kTile, kSquareA>(a, batch, st)) != hipSuccess) return e;
+    if ((e = product<float, kTile, kPlanes, kSquareA>(a, batch, st)) != hipSuccess) return e;
     a.P = B;
     a.Q = a.add = now;
     a.out = next;
     a.out2 = X;
     a.tj = l.s.np / kTile;
-    e = last ? product<T, kTile, kApplyLast>(a, batch, st) : product<float, kTile, kApplyB>(a, batch, st);
+    e = last ? product<T, kTile, kPlanes, kApplyLast>(a, batch, st) : product<float, kTile, kPlanes, kApplyB>(a, batch, st);
     if (e != hipSuccess) return e;
     std::swap(now, next);
   }
@@ -338,6 +599,13 @@ hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, cha
 template <class T>
 hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t rows, int64_t cols, int steps,
                          float eps, char* work, hipStream_t st) {
+  if (l.tiny) {
+    const hipError_t e = allow_lds<k_orth_tiny<T>>((int)kTinyLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_orth_tiny<T>), dim3((unsigned)batch), dim3(kTinyThreads), kTinyLds, st, u, (int)rows,
+                       (int)cols, l.s.turned, steps, eps);
+    return hipGetLastError();
+  }
   _Float16* at = reinterpret_cast<_Float16*>(work);
   const auto planes = [&](int64_t elems, int ld) {
     Planes p;
@@ -351,16 +619,19 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   const Planes X = planes(l.xs, l.s.np), XT0 = planes(l.xs, l.s.mp), XT1 = planes(l.xs, l.s.mp),
                A = planes(l.as, l.s.mp), B = planes(l.as, l.s.mp);
   double* sums = reinterpret_cast<double*>(work + l.sums);
-  const int nsums = (int)std::min<int64_t>(rows, kNormBlocks);
-  hipLaunchKernelGGL((k_orth_norm<T>), dim3(nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
+  hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int pr = l.s.turned ? l.s.np : l.s.mp, pc = l.s.turned ? l.s.mp : l.s.np;  // G's sides, padded
   hipLaunchKernelGGL((k_orth_begin<T>), dim3(pc / 64, pr / 64, (unsigned)batch), dim3(kThreads), 0, st, u, l.s, sums,
-                     nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0, (int)rows, (int)cols);
+                     l.nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0, (int)rows, (int)cols);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  return l.tile == 128 ? iterate<T, 128>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
-                       : iterate<T, 64>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
+  if constexpr (std::is_same<T, bf16>::value)
+    if (l.s.m > kSmall)
+      return l.tile == 128 ? iterate<T, 128, 1>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
+                           : iterate<T, 64, 1>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
+  return l.tile == 128 ? iterate<T, 128, 2>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
+                       : iterate<T, 64, 2>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
 }
 
 int check_sizes(int64_t batch, int64_t rows, int64_t cols) {
@@ -403,7 +674,7 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
   if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))
     return op_error(MLKV_EINVAL, "out may be g only with the same strides");
   const Layout l = layout(batch, rows, cols);
-  if (d_work == nullptr || work_bytes < l.bytes)
+  if (l.bytes > 0 && (d_work == nullptr || work_bytes < l.bytes))
     return op_error(MLKV_EINVAL, "work is smaller than mlkv_orthogonalize_workspace");
   if (!all_aligned(256, 1, {d_work}, {})) return op_error(MLKV_EINVAL, "work must be at a multiple of 256 bytes");
   User u;

@@ -269,7 +269,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
         out = _out(out, "out", g)
         ob, orow = _matrices(out, "out")
         nbytes = _bytes(mlkv.mlkv_orthogonalize_workspace(batch, rows, cols))
-        work = torch.empty(nbytes, dtype=torch.uint8, device=g.device)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=g.device) if nbytes else None
         mlkv._check(mlkv.mlkv_orthogonalize(g, gb, gr, batch, rows, cols, int(steps), eps, kind, out, ob, orow, work,
                                             nbytes, st))
     return out

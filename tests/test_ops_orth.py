@@ -78,7 +78,7 @@ def update(gen, *shape, kind=torch.float32, scale=0.01):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (9, 1), (2, 2), (3, 64), (63, 65), (64, 64), (65, 63), (64, 250),
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (9, 1), (2, 2), (3, 64), (63, 65), (64, 64), (65, 63), (64, 250), (64, 256), (64, 257), (66, 250),
                                        (250, 64), (127, 129), (128, 128), (200, 1000), (1000, 200), (513, 511)])
 def test_shapes(gen, rows, cols, kind):
     check(update(gen, rows, cols, kind=kind))
@@ -191,8 +191,8 @@ def test_streams_and_graph_replays(gen):
 
 # ---- refusals (no GPU needed: nothing is launched) ----
 def call(**change):
-    a = dict(g=4096, gb=6400, gr=100, batch=2, rows=64, cols=100, steps=5, eps=1e-7, dtype=mlkv.MLKV_F32, out=2 ** 20,
-             ob=6400, orow=100, work=2 ** 24, bytes=2 ** 24)
+    a = dict(g=4096, gb=6600, gr=100, batch=2, rows=66, cols=100, steps=5, eps=1e-7, dtype=mlkv.MLKV_F32, out=2 ** 20,
+             ob=6600, orow=100, work=2 ** 24, bytes=2 ** 24)
     a.update(change)
     return mlkv.mlkv_orthogonalize(a["g"], a["gb"], a["gr"], a["batch"], a["rows"], a["cols"], a["steps"], a["eps"],
                                    a["dtype"], a["out"], a["ob"], a["orow"], a["work"], a["bytes"], 0)
@@ -203,7 +203,7 @@ def call(**change):
     (dict(cols=32769), "rows and cols"), (dict(steps=0), "steps"), (dict(steps=65), "steps"), (dict(eps=0.0), "eps"),
     (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(dtype=3), "dtype"), (dict(g=None), "NULL"),
     (dict(out=None), "NULL"), (dict(gr=99), "row strides"), (dict(orow=0), "row strides"), (dict(gb=-1), "overlap"),
-    (dict(ob=6399), "overlap"), (dict(ob=0), "overlap"), (dict(out=4096, orow=101, ob=6464), "same strides"),
+    (dict(ob=6599), "overlap"), (dict(ob=0), "overlap"), (dict(out=4096, orow=101, ob=6666), "same strides"),
     (dict(work=None), "work"), (dict(bytes=1000), "work"), (dict(work=2 ** 24 + 128), "work"),
     (dict(g=4097), "aligned"), (dict(out=2 ** 20 + 2), "aligned")])
 def test_refusals(change, says):
@@ -213,7 +213,7 @@ def test_refusals(change, says):
 
 def test_workspace_sizes():
     size = mlkv.mlkv_orthogonalize_workspace
-    assert size(0, 5, 5) == 0 and size(1, 64, 64) > 0
+    assert size(0, 5, 5) == 0 and size(1, 66, 65) > 0
     assert size(1, 100, 70) == size(1, 70, 100)
     for bad in ((-1, 5, 5), (1, 0, 5), (1, 5, 32769), (65536, 1, 1)):
         assert size(*bad) == mlkv.MLKV_EINVAL
