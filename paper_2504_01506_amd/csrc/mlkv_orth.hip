@@ -331,15 +331,18 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
       }
 }
 
-// ---- small matrices: all steps in one block ----
-// Matrices of at most 64 x 256 (as iterated on) live in LDS, X and X^T as
-// pairs, A, and B in the place of X X^T's second half sums: all 160 KB of a
-// unit. Eight waves: X X^T a block of 32 x 32 and half the sum each, A A the
-// blocks, B X 32 columns each. Bound by the latency of its chain: three products
-// and four exchanges through LDS a step.
-constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
-constexpr int kTinyX = kTinyM * kTinyN, kTinyA = kTinyM * kTinyM;  // halves of a plane
-constexpr size_t kTinyLds = sizeof(_Float16) * (4 * kTinyX + 4 * kTinyA);
+// ---- matrices of few rows: panels in LDS ----
+// Matrices of at most 64 rows (as iterated on) are cut into panels of 256
+// columns. A block holds one in LDS, X and X^T as pairs, A, and B in the place
+// of X X^T's second half sums: all 160 KB of a unit. Eight waves: X X^T a block
+// of 32 x 32 and half the sum each, A A the blocks, B X 32 columns each. A
+// matrix of one panel takes all steps in one launch; of several, a launch a
+// step, in which every block joins all panels' X X^T and works out A and B for
+// itself. Bound by the latency of the chain, three products and four exchanges
+// through LDS a step (4 to 6 us).
+constexpr int kPanelRows = 64, kPanelCols = 256, kPanelThreads = 512;
+constexpr int kPanelX = kPanelRows * kPanelCols, kPanelA = kPanelRows * kPanelRows;  // halves of a plane
+constexpr size_t kPanelLds = sizeof(_Float16) * (4 * kPanelX + 4 * kPanelA);
 
 // Element k of row r of a plane with rows of kRow halves. Pieces of 16 bytes are
 // exchanged by the row, so that 8 lanes that read a column of pieces meet 8
@@ -347,49 +350,74 @@ constexpr size_t kTinyLds = sizeof(_Float16) * (4 * kTinyX + 4 * kTinyA);
 template <int kRow>
 __device__ __forceinline__ int spot(int r, int k) { return r * kRow + (((k >> 3) ^ (r & 7)) << 3) + (k & 7); }
 
-template <class T>
-__global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, int cols, bool turned, int steps,
-                                                            float eps) {
-  extern __shared__ __align__(16) _Float16 lds_tiny[];
-  _Float16* X = lds_tiny;                // [2][64][256]
-  _Float16* XT = X + 2 * kTinyX;         // [2][256][64]
-  _Float16* A = XT + 2 * kTinyX;         // [2][64][64]
-  _Float16* B = A + 2 * kTinyA;          // [2][64][64]
+// What a step's launch leaves to the next (matrices of several panels).
+struct PanelWork {
+  _Float16* xt;        // [batch][panels][2][256][64]: X^T, as it lies in LDS
+  float4* sums;        // [batch][2 turns][panels][2 halves][4 blocks][4][64 lanes]: X X^T
+  const double* norm;  // [batch][nsums]
+  int nsums;
+};
+
+// kWhole: a matrix's only panel, all steps. kFirst: X and its X X^T. kNext: one step.
+enum PanelStep : int { kWhole, kFirst, kNext };
+template <class T, int kStep>
+__global__ __launch_bounds__(kPanelThreads) void k_orth_panel(User u, PanelWork w, int rows, int cols, bool turned,
+                                                             int steps, float eps, int turn, bool last) {
+  constexpr int kSums = 4 * 4 * 64;  // float4s of the sums of half a panel
+  extern __shared__ __align__(16) _Float16 panel_lds[];
+  _Float16* X = panel_lds;                // [2][64][256]
+  _Float16* XT = X + 2 * kPanelX;         // [2][256][64]
+  _Float16* A = XT + 2 * kPanelX;         // [2][64][64]
+  _Float16* B = A + 2 * kPanelA;          // [2][64][64]
   float4* half = reinterpret_cast<float4*>(B);  // [4 blocks][4][64 lanes]: the sums' second halves, before B
   double* part = reinterpret_cast<double*>(A);  // [8], before A
   int lane = threadIdx.x & 63;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const T* g = static_cast<const T*>(u.g) + blockIdx.x * u.g_batch;
-  const int m = turned ? cols : rows, n = turned ? rows : cols;
+  const int m = turned ? cols : rows, n_all = turned ? rows : cols;
+  const int panel = blockIdx.x, panels = gridDim.x, from = panel * kPanelCols, n = min(n_all - from, kPanelCols);
+  _Float16* keep = kStep == kWhole ? nullptr : w.xt + ((int64_t)blockIdx.y * panels + panel) * 2 * kPanelX;
+  float4* sums = kStep == kWhole ? nullptr : w.sums + (int64_t)blockIdx.y * 2 * panels * 2 * kSums;
+  if constexpr (kStep == kNext) {
+#pragma unroll
+    for (int e = 0; e < 2 * kPanelX / 8 / kPanelThreads; ++e)
+      reinterpret_cast<Raw*>(XT)[e * kPanelThreads + tid] = reinterpret_cast<const Raw*>(keep)[e * kPanelThreads + tid];
+  } else {
+    const T* g = static_cast<const T*>(u.g) + blockIdx.y * u.g_batch + (turned ? from * u.g_row : from);
+    const int g_rows = turned ? n : rows, g_cols = turned ? cols : n;
 
-  // G's rows along the threads: 64 x 256, or 256 x 64 where it is turned
-  constexpr int kEach = kTinyX / kTinyThreads;
-  const int wide = turned ? 6 : 8;  // log2 of that
-  float v[kEach];
-  double t = 0.0;
+    // G's rows along the threads: 64 x 256, or 256 x 64 where it is turned
+    constexpr int kEach = kPanelX / kPanelThreads;
+    const int wide = turned ? 6 : 8;  // log2 of that
+    float v[kEach];
+    double t = 0.0;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int at = e * kTinyThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
-    v[e] = r < rows && c < cols ? (float)g[r * u.g_row + c] : 0.0f;
-  }
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * kPanelThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
+      v[e] = r < g_rows && c < g_cols ? (float)g[r * u.g_row + c] : 0.0f;
+    }
+    if constexpr (kStep == kWhole) {
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) t = __builtin_fma((double)v[e], (double)v[e], t);
-  for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
-  if (lane == 0) part[wave] = t;
-  __syncthreads();
-  t = 0.0;
-  for (int w = 0; w < kTinyThreads / 64; ++w) t += part[w];
-  const double inv = 32768.0 / (sqrt(t) + (double)eps);
+      for (int e = 0; e < kEach; ++e) t = __builtin_fma((double)v[e], (double)v[e], t);
+    } else {
+      for (int k = tid; k < w.nsums; k += kPanelThreads) t += w.norm[(int64_t)blockIdx.y * w.nsums + k];
+    }
+    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+    if (lane == 0) part[wave] = t;
+    __syncthreads();
+    t = 0.0;
+    for (int k = 0; k < kPanelThreads / 64; ++k) t += part[k];
+    const double inv = 32768.0 / (sqrt(t) + (double)eps);
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int at = e * kTinyThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
-    const int i = turned ? c : r, j = turned ? r : c;
-    _Float16 hi, lo;
-    split((float)((double)v[e] * inv), hi, lo);
-    X[spot<kTinyN>(i, j)] = hi;
-    X[kTinyX + spot<kTinyN>(i, j)] = lo;
-    XT[spot<kTinyM>(j, i)] = hi;
-    XT[kTinyX + spot<kTinyM>(j, i)] = lo;
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * kPanelThreads + tid, r = at >> wide, c = at & ((1 << wide) - 1);
+      const int i = turned ? c : r, j = turned ? r : c;
+      _Float16 hi, lo;
+      split((float)((double)v[e] * inv), hi, lo);
+      X[spot<kPanelCols>(i, j)] = hi;
+      X[kPanelX + spot<kPanelCols>(i, j)] = lo;
+      XT[spot<kPanelRows>(j, i)] = hi;
+      XT[kPanelX + spot<kPanelRows>(j, i)] = lo;
+    }
   }
   __syncthreads();
 
@@ -444,17 +472,51 @@ __global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, in
     fours(bi * 32, bj * 32, [&](int i, int j, int e) {
       half4 hi, lo;
       halves(x, e, hi, lo);
-      *reinterpret_cast<half4*>(to + spot<kTinyM>(j, i)) = hi;
-      *reinterpret_cast<half4*>(to + kTinyA + spot<kTinyM>(j, i)) = lo;
+      *reinterpret_cast<half4*>(to + spot<kPanelRows>(j, i)) = hi;
+      *reinterpret_cast<half4*>(to + kPanelA + spot<kPanelRows>(j, i)) = lo;
     });
   };
-  using OfX = std::integral_constant<int, kTinyN>;
-  using OfA = std::integral_constant<int, kTinyM>;
+  using OfX = std::integral_constant<int, kPanelCols>;
+  using OfA = std::integral_constant<int, kPanelRows>;
   // pieces of the sum over n: an even number for each half, those behind n of zeros
   const int each = ((n + 15) / 16 + 3) / 4 * 2;
+  const auto square = [&] {
+    return multiply(OfX{}, X, bi * 32, X, bj * 32, kPanelX, kPanelX, second ? each * 16 : 0, each);
+  };
+  // the panel for the next launch: its X X^T, by halves, and X^T
+  const auto leave = [&](int to) {
+    const float16v s = square();
+    float4* at = sums + ((int64_t)(to * panels + panel) * 2 + second) * kSums + (wave & 3) * 4 * 64 + lane;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) at[e * 64] = make_float4(s[e * 4], s[e * 4 + 1], s[e * 4 + 2], s[e * 4 + 3]);
+#pragma unroll
+    for (int e = 0; e < 2 * kPanelX / 8 / kPanelThreads; ++e)
+      reinterpret_cast<Raw*>(keep)[e * kPanelThreads + tid] = reinterpret_cast<const Raw*>(XT)[e * kPanelThreads + tid];
+  };
+  if constexpr (kStep == kFirst) {
+    leave(0);
+    return;
+  }
   for (int step = 0; step < steps; ++step) {
     asm volatile("" : "+v"(lane));  // (places in LDS are worked out again: kept over the steps they take all registers)
-    float16v s = multiply(OfX{}, X, bi * 32, X, bj * 32, kTinyX, kTinyX, second ? each * 16 : 0, each);
+    float16v s;
+    if constexpr (kStep == kWhole) {
+      s = square();
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+      const float4* at = sums + ((int64_t)turn * panels * 2 + second) * kSums + (wave & 3) * 4 * 64 + lane;
+#pragma unroll 2
+      for (int k = 0; k < panels; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 x = at[(int64_t)k * 2 * kSums + e * 64];
+          s[e * 4] += x.x;
+          s[e * 4 + 1] += x.y;
+          s[e * 4 + 2] += x.z;
+          s[e * 4 + 3] += x.w;
+        }
+    }
     if (second) {
 #pragma unroll
       for (int e = 0; e < 16; e += 4)
@@ -474,7 +536,7 @@ __global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, in
     }
     __syncthreads();
     if (!second) {
-      const float16v q = multiply(OfA{}, A, bi * 32, A, bj * 32, kTinyA, kTinyA, 0, 4);
+      const float16v q = multiply(OfA{}, A, bi * 32, A, bj * 32, kPanelA, kPanelA, 0, 4);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(kC * 0x1p-16f, q[e], kB * 0.5f * s[e]);
       put(B, s);
@@ -482,32 +544,33 @@ __global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, in
     __syncthreads();
     // the wave's 32 columns; no other wave reads their rows of X^T, and none X
     const int j0 = wave * 32;
-    if (j0 < n) {
+    if (kStep == kNext || j0 < n) {  // (columns behind n: zeros, which a panel keeps)
       float16v y[2];  // both are computed before either is written
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        y[x] = multiply(OfA{}, B, x * 32, XT, j0, kTinyA, kTinyX, 0, 4);
+        y[x] = multiply(OfA{}, B, x * 32, XT, j0, kPanelA, kPanelX, 0, 4);
         fours(x * 32, j0, [&](int i, int j, int e) {
-          const half4 hi = *reinterpret_cast<const half4*>(XT + spot<kTinyM>(j, i));
-          const half4 lo = *reinterpret_cast<const half4*>(XT + kTinyX + spot<kTinyM>(j, i));
+          const half4 hi = *reinterpret_cast<const half4*>(XT + spot<kPanelRows>(j, i));
+          const half4 lo = *reinterpret_cast<const half4*>(XT + kPanelX + spot<kPanelRows>(j, i));
 #pragma unroll
           for (int d = 0; d < 4; ++d)
             y[x][e + d] = __builtin_fmaf(0x1p-14f, y[x][e + d], kA * ((float)hi[d] + (float)lo[d]));
         });
       }
-      T* out = static_cast<T*>(u.out) + blockIdx.x * u.o_batch;
+      const bool ends = kStep == kWhole ? step + 1 == steps : last;
+      T* out = static_cast<T*>(u.out) + blockIdx.y * u.o_batch + (turned ? from * u.o_row : from);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
         fours(x * 32, j0, [&](int i, int j, int e) {
-          if (step + 1 < steps) {
+          if (!ends) {
             half4 hi, lo;
             halves(y[x], e, hi, lo);
-            *reinterpret_cast<half4*>(XT + spot<kTinyM>(j, i)) = hi;
-            *reinterpret_cast<half4*>(XT + kTinyX + spot<kTinyM>(j, i)) = lo;
+            *reinterpret_cast<half4*>(XT + spot<kPanelRows>(j, i)) = hi;
+            *reinterpret_cast<half4*>(XT + kPanelX + spot<kPanelRows>(j, i)) = lo;
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-              X[spot<kTinyN>(i + d, j)] = hi[d];
-              X[kTinyX + spot<kTinyN>(i + d, j)] = lo[d];
+              X[spot<kPanelCols>(i + d, j)] = hi[d];
+              X[kPanelX + spot<kPanelCols>(i + d, j)] = lo[d];
             }
           } else if (j < n) {
 #pragma unroll
@@ -518,6 +581,10 @@ __global__ __launch_bounds__(kTinyThreads) void k_orth_tiny(User u, int rows, in
         });
     }
     __syncthreads();
+    if constexpr (kStep == kNext) {
+      if (!last) leave(turn ^ 1);
+      return;
+    }
   }
 }
 
@@ -527,7 +594,7 @@ struct Layout {
   int64_t xs, as;  // elements of a plane of X and of A
   int64_t sums, bytes;  // offset of the sums of squares; all
   int nsums;            // of a matrix
-  bool tiny;            // one block a matrix, no workspace
+  int panels;           // of a matrix of few rows, or 0
 };
 
 // Tiles of 128 unless they are fewer than the device's units.
@@ -538,9 +605,13 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   l.s.n = (int)std::max(rows, cols);
   const auto up = [](int64_t v, int64_t t) { return (v + t - 1) / t * t; };
   const int64_t t128 = up(l.s.m, 128) / 128;
-  l.tiny = l.s.m <= kTinyM && l.s.n <= kTinyN;
-  if (l.tiny) {
-    l.bytes = 0;
+  l.nsums = (int)std::min<int64_t>((rows + 3) / 4, kNormBlocks);
+  // (as many bytes for a matrix as for its transpose)
+  const int64_t sums = batch * std::min<int64_t>((l.s.n + 3) / 4, kNormBlocks) * (int64_t)sizeof(double);
+  l.panels = l.s.m <= kPanelRows ? (l.s.n + kPanelCols - 1) / kPanelCols : 0;
+  if (l.panels > 0) {
+    l.sums = batch * l.panels * (int64_t)(sizeof(_Float16) * 2 * kPanelX + sizeof(float4) * 4096);
+    l.bytes = l.panels == 1 ? 0 : l.sums + sums;
     return l;
   }
   l.tile = batch * t128 * (t128 + 1) / 2 >= 256 ? 128 : 64;
@@ -551,9 +622,7 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   // X, two of X^T, A and B, two planes each
   l.sums = batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16);
   l.sums = up(l.sums, 256);
-  l.nsums = (int)std::min<int64_t>((rows + 3) / 4, kNormBlocks);
-  // (as many bytes for a matrix as for its transpose)
-  l.bytes = l.sums + batch * std::min<int64_t>((l.s.n + 3) / 4, kNormBlocks) * (int64_t)sizeof(double);
+  l.bytes = l.sums + sums;
   return l;
 }
 
@@ -596,16 +665,38 @@ hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, cha
   return hipSuccess;
 }
 
+template <class T, int kStep>
+hipError_t panel_step(const Layout& l, const User& u, const PanelWork& w, int64_t batch, int64_t rows, int64_t cols,
+                      int steps, float eps, int turn, bool last, hipStream_t st) {
+  const hipError_t e = allow_lds<k_orth_panel<T, kStep>>((int)kPanelLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_orth_panel<T, kStep>), dim3((unsigned)l.panels, (unsigned)batch), dim3(kPanelThreads), kPanelLds,
+                     st, u, w, (int)rows, (int)cols, l.s.turned, steps, eps, turn, last);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t panel_steps(const Layout& l, const User& u, int64_t batch, int64_t rows, int64_t cols, int steps, float eps,
+                       char* work, hipStream_t st) {
+  PanelWork w{};
+  if (l.panels == 1) return panel_step<T, kWhole>(l, u, w, batch, rows, cols, steps, eps, 0, true, st);
+  double* norm = reinterpret_cast<double*>(work + l.sums);
+  w.sums = reinterpret_cast<float4*>(work);
+  w.xt = reinterpret_cast<_Float16*>(work + batch * l.panels * (int64_t)sizeof(float4) * 4096);
+  w.norm = norm;
+  w.nsums = l.nsums;
+  hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, norm);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) e = panel_step<T, kFirst>(l, u, w, batch, rows, cols, 1, eps, 0, false, st);
+  for (int k = 0; k < steps && e == hipSuccess; ++k)
+    e = panel_step<T, kNext>(l, u, w, batch, rows, cols, 1, eps, k & 1, k + 1 == steps, st);
+  return e;
+}
+
 template <class T>
 hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t rows, int64_t cols, int steps,
                          float eps, char* work, hipStream_t st) {
-  if (l.tiny) {
-    const hipError_t e = allow_lds<k_orth_tiny<T>>((int)kTinyLds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_orth_tiny<T>), dim3((unsigned)batch), dim3(kTinyThreads), kTinyLds, st, u, (int)rows,
-                       (int)cols, l.s.turned, steps, eps);
-    return hipGetLastError();
-  }
+  if (l.panels > 0) return panel_steps<T>(l, u, batch, rows, cols, steps, eps, work, st);
   _Float16* at = reinterpret_cast<_Float16*>(work);
   const auto planes = [&](int64_t elems, int ld) {
     Planes p;

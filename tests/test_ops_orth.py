@@ -79,6 +79,7 @@ def update(gen, *shape, kind=torch.float32, scale=0.01):
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (9, 1), (2, 2), (3, 64), (63, 65), (64, 64), (65, 63), (64, 250), (64, 256), (64, 257), (66, 250),
+                                       (326, 40), (7, 4096), (64, 1111), (1537, 33), (1, 700),
                                        (250, 64), (127, 129), (128, 128), (200, 1000), (1000, 200), (513, 511)])
 def test_shapes(gen, rows, cols, kind):
     check(update(gen, rows, cols, kind=kind))
@@ -86,7 +87,7 @@ def test_shapes(gen, rows, cols, kind):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch,rows,cols", [(1, 40, 50), (7, 33, 90), (16, 64, 250), (3, 300, 130), (130, 60, 20),
-                                             (40, 384, 384)])
+                                             (40, 384, 384), (5, 48, 700), (70, 600, 16)])
 def test_stacks(gen, batch, rows, cols):
     check(update(gen, batch, rows, cols))
     check(update(gen, batch, rows, cols, kind=torch.bfloat16))
