@@ -30,7 +30,7 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kThreads = 256;
-constexpr int kDepth = 32;       // k of a stage: 64 bytes a row and plane
+constexpr int kPad = 64;         // sides of X and A are padded to multiples of it, with zeros
 constexpr int kNormBlocks = 512; // sums of squares a matrix, at most
 constexpr int kSmall = 128;
 
@@ -40,7 +40,7 @@ using float16v = float __attribute__((ext_vector_type(16)));
 
 struct Shape {
   int m, n;    // as iterated on: m <= n
-  int mp, np;  // padded to whole tiles, zeros in the padding
+  int mp, np;  // padded, zeros in the padding
   bool turned; // rows > cols
 };
 
@@ -114,6 +114,7 @@ struct Planes {
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const double* sums, int nsums, float eps,
                                                          Planes straight, Planes turned, int rows, int cols) {
+  const int pr = s.turned ? s.np : s.mp, pc = s.turned ? s.mp : s.np;  // G's sides, padded
   __shared__ float tile[64][65];
   __shared__ double part[kThreads / 64];
   double t = 0.0;
@@ -134,8 +135,10 @@ __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const 
     _Float16 hi, lo;
     split(v, hi, lo);
     const int64_t at = (int64_t)r * straight.ld + c;
-    a[at] = hi;
-    a[straight.plane + at] = lo;
+    if (r < pr && c < pc) {
+      a[at] = hi;
+      a[straight.plane + at] = lo;
+    }
   }
   __syncthreads();
   _Float16* b = turned.p + blockIdx.z * turned.batch;
@@ -143,8 +146,10 @@ __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const 
     _Float16 hi, lo;
     split(tile[tx][y], hi, lo);
     const int64_t at = (int64_t)(c0 + y) * turned.ld + r0 + tx;
-    b[at] = hi;
-    b[turned.plane + at] = lo;
+    if (c0 + y < pc && r0 + tx < pr) {
+      b[at] = hi;
+      b[turned.plane + at] = lo;
+    }
   }
 }
 
@@ -165,27 +170,47 @@ struct ProdArgs {
 using lds_ptr = __attribute__((address_space(3))) void*;
 using global_ptr = const __attribute__((address_space(1))) void*;
 
-// Row r's 16-byte piece c of a stage lies at piece c ^ ((r >> 1) & 3): the 8
-// lanes that LDS serves at a time then read 8 different bank groups.
-__device__ __forceinline__ int piece(int r, int c) { return r * kDepth + ((c ^ (r >> 1)) & 3) * 8; }
-
-// Waits until at most kLater of the wave's loads are in flight, then for the
-// block's other waves.
-template <int kLater>
-__device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLater) : "memory");
+// Element of a stage, with rows of kDepth halves, where row r's 16-byte piece c
+// lies: pieces are exchanged by the row, so that the 8 lanes that LDS serves at
+// a time read 8 different bank groups.
+template <int kDepth>
+__device__ __forceinline__ int piece(int r, int c) {
+  return kDepth == 32 ? r * 32 + ((c ^ (r >> 1)) & 3) * 8 : r * 64 + ((c ^ r) & 7) * 8;
 }
 
-// A tile of kTile x kTile by four waves, a quarter each, in blocks of 32 x 32.
-// kStages stages of kDepth in LDS: while one is multiplied, the others are on
-// their way from memory. 64 KB, so that two blocks run on a unit.
-template <class T, int kTile, int kPlanes, int kStep>
-__global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
-  constexpr int kBlocks = kTile / 64;
+// Waits until at most kLater of the wave's loads are in flight and its reads of
+// LDS are done, then for the block's other waves.
+template <int kLater>
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
+}
+
+// A square tile of C, kSide a side, and its waves: kI x kJ that share it in
+// equal parts, or (kK > 1) kK that each have all of it for every kK-th piece of
+// 16 of k and join their sums at the end. Blocks of 32 x 32; kBytes of LDS for
+// stages of kDepth. A small tile in parts reads four pieces of LDS for three
+// products and waits for each in turn; by pieces of k it reads eight for twelve.
+template <int kSide, int kI, int kJ, int kK, int kDepth_, int kBytes>
+struct Tile {
+  static_assert(kK == 1 || (kI == 1 && kJ == 1 && kK == 4 && kSide == 64), "four waves, a block of the sum each");
+  static constexpr int side = kSide, depth = kDepth_, lds = kBytes, waves_k = kK, waves = kI * kJ * kK;
+  static constexpr int blocks_i = kSide / kI / 32, blocks_j = kSide / kJ / 32;  // of a wave
+  static constexpr int across = kK > 1 ? 2 : kJ;                               // waves along j of the result
+  static constexpr int out_i = kK > 1 ? 1 : blocks_i, out_j = kK > 1 ? 1 : blocks_j;
+};
+
+// kStages stages in LDS: while one is multiplied, the others are on their way
+// from memory.
+template <class T, class Tile_, int kPlanes, int kStep>
+__global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) {
+  constexpr int kTile = Tile_::side, kDepth = Tile_::depth, kWaves = Tile_::waves;
+  constexpr int kBi = Tile_::blocks_i, kBj = Tile_::blocks_j, kOi = Tile_::out_i, kOj = Tile_::out_j;
   constexpr int kStage = 2 * kPlanes * kTile * kDepth;  // halves
-  constexpr int kStages = 65536 / (int)(kStage * sizeof(_Float16));
-  constexpr int kLoads = 2 * kPlanes * kTile / 16 / 4;  // of a wave and stage
-  __shared__ __align__(16) _Float16 lds[kStages * kStage];
+  constexpr int kStages = Tile_::lds / (int)(kStage * sizeof(_Float16));
+  constexpr int kRows = 512 / kDepth;                   // rows of a load: a kilobyte
+  constexpr int kLoads = 2 * kPlanes * kTile / kRows / kWaves;  // of a wave and stage
+  static_assert(kStages >= 2 && 2 * kPlanes * kTile / kRows % kWaves == 0, "stages and loads");
+  extern __shared__ __align__(16) _Float16 lds[];
   constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // neighbouring tiles on one XCD (blocks go round the 8 in turn), for its L2
@@ -204,68 +229,156 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
     bj = in / high;
     bi = band * 8 + in - bj * high;
   }
-  const _Float16* P = a.P.p + blockIdx.z * a.P.batch + (int64_t)bi * kTile * a.P.ld;
-  const _Float16* Q = a.Q.p + blockIdx.z * a.Q.batch + (int64_t)bj * kTile * a.Q.ld;
+  const int rows_i = a.s.mp, rows_j = kSym ? a.s.mp : a.s.np;
 
-  // 16 rows of a plane a load: lane l fetches piece (l & 3) ^ ... of row l / 4
+  // A load takes kRows rows of a plane, a lane a piece. Rows that a tile has
+  // beyond the matrix are read as its last.
+  constexpr int kLanes = 64 / kRows;  // of a row
   const _Float16* from[kLoads];
 #pragma unroll
   for (int q = 0; q < kLoads; ++q) {
-    const int seg = q * 4 + wave, plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
-    const Planes& o = plane < kPlanes ? a.P : a.Q;
-    from[q] = (plane < kPlanes ? P : Q) + (plane % kPlanes) * o.plane + (int64_t)(rows + lane / 4) * o.ld +
-              (((lane & 3) ^ (lane >> 3)) & 3) * 8;
+    const int seg = q * kWaves + wave, plane = seg / (kTile / kRows), rows = seg % (kTile / kRows) * kRows;
+    const bool is_p = plane < kPlanes;
+    const Planes& o = is_p ? a.P : a.Q;
+    const int in = rows + lane / kLanes, r = min((is_p ? bi : bj) * kTile + in, (is_p ? rows_i : rows_j) - 1);
+    from[q] = o.p + blockIdx.z * o.batch + (plane % kPlanes) * o.plane + (int64_t)r * o.ld +
+              (piece<kDepth>(in, lane % kLanes) - in * kDepth);
   }
   const auto fill = [&](int t) {
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
-      const int seg = q * 4 + wave, plane = seg / (kTile / 16), rows = seg % (kTile / 16) * 16;
+      const int seg = q * kWaves + wave, plane = seg / (kTile / kRows), rows = seg % (kTile / kRows) * kRows;
       _Float16* to = lds + (t % kStages) * kStage + plane * kTile * kDepth + rows * kDepth;
       __builtin_amdgcn_global_load_lds((global_ptr)(from[q] + t * kDepth), (lds_ptr)to, 16, 0, 0);
     }
   };
 
-  float16v acc[kBlocks][kBlocks];
+  float16v acc[kBi][kBj];
 #pragma unroll
-  for (int x = 0; x < kBlocks; ++x)
+  for (int x = 0; x < kBi; ++x)
 #pragma unroll
-    for (int y = 0; y < kBlocks; ++y)
+    for (int y = 0; y < kBj; ++y)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
 
-  const int wi = (wave >> 1) * (kTile / 2), wj = (wave & 1) * (kTile / 2);
+  const int wi = Tile_::waves_k > 1 ? 0 : wave / Tile_::across * (kBi * 32);
+  const int wj = Tile_::waves_k > 1 ? 0 : wave % Tile_::across * (kBj * 32);
   const int stages = a.k / kDepth;
 #pragma unroll
   for (int t = 0; t < kStages - 1; ++t)
     if (t < stages) fill(t);
-  for (int t = 0; t < stages; ++t) {
-    // stage t is there, and all waves are done with stage t - 1, whose place is filled next
+  // stage t is there, and all waves are done reading stage t - 1, whose place is filled next
+  const auto next_stage = [&](int t) {
     if (t + kStages - 2 < stages) stage_barrier<(kStages - 2) * kLoads>();
     else stage_barrier<0>();
     if (t + kStages - 1 < stages) fill(t + kStages - 1);
+  };
+  struct Pieces {
+    half8 p[kBi][kPlanes], q[kBj][kPlanes];
+  };
+  const auto read = [&](Pieces& s, int t, int h) {
     const _Float16* st = lds + (t % kStages) * kStage;
+    const int c = (Tile_::waves_k > 1 ? h * Tile_::waves_k + wave : h) * 2 + lane / 32;
 #pragma unroll
-    for (int h = 0; h < kDepth / 16; ++h) {
-      half8 p[kBlocks][kPlanes], q[kBlocks][kPlanes];
-      const int c = h * 2 + lane / 32;
+    for (int e = 0; e < kPlanes; ++e) {
 #pragma unroll
-      for (int x = 0; x < kBlocks; ++x)
+      for (int x = 0; x < kBi; ++x)
+        s.p[x][e] = *reinterpret_cast<const half8*>(st + e * kTile * kDepth +
+                                                    piece<kDepth>(wi + x * 32 + (lane & 31), c));
 #pragma unroll
-        for (int e = 0; e < kPlanes; ++e) {
-          p[x][e] = *reinterpret_cast<const half8*>(st + e * kTile * kDepth + piece(wi + x * 32 + (lane & 31), c));
-          q[x][e] = *reinterpret_cast<const half8*>(st + (kPlanes + e) * kTile * kDepth +
-                                                    piece(wj + x * 32 + (lane & 31), c));
-        }
+      for (int y = 0; y < kBj; ++y)
+        s.q[y][e] = *reinterpret_cast<const half8*>(st + (kPlanes + e) * kTile * kDepth +
+                                                    piece<kDepth>(wj + y * 32 + (lane & 31), c));
+    }
+  };
+  const auto multiply = [&](const Pieces& s) {
 #pragma unroll
-      for (int x = 0; x < kBlocks; ++x)
+    for (int x = 0; x < kBi; ++x)
 #pragma unroll
-        for (int y = 0; y < kBlocks; ++y) {
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][0], acc[x][y], 0, 0, 0);
-          if constexpr (kPlanes == 2) {
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][0], q[y][1], acc[x][y], 0, 0, 0);
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[x][1], q[y][0], acc[x][y], 0, 0, 0);
-          }
-        }
+      for (int y = 0; y < kBj; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][0], s.q[y][0], acc[x][y], 0, 0, 0);
+    if constexpr (kPlanes == 2) {
+#pragma unroll
+      for (int x = 0; x < kBi; ++x)
+#pragma unroll
+        for (int y = 0; y < kBj; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][0], s.q[y][1], acc[x][y], 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < kBi; ++x)
+#pragma unroll
+        for (int y = 0; y < kBj; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][1], s.q[y][0], acc[x][y], 0, 0, 0);
+    }
+  };
+  if constexpr (Tile_::waves_k > 1) {
+    // a wave has one piece of a stage: it reads the next while it multiplies this one
+    static_assert(kDepth / 16 == Tile_::waves_k, "a piece a wave and stage");
+    Pieces s[2];
+    next_stage(0);
+    read(s[0], 0, 0);
+    int t = 1;
+    for (; t + 1 < stages; t += 2) {
+      next_stage(t);
+      read(s[1], t, 0);
+      multiply(s[0]);
+      next_stage(t + 1);
+      read(s[0], t + 1, 0);
+      multiply(s[1]);
+    }
+    if (t < stages) {
+      next_stage(t);
+      read(s[1], t, 0);
+      multiply(s[0]);
+      multiply(s[1]);
+    } else {
+      multiply(s[0]);
+    }
+  } else {
+    for (int t = 0; t < stages; ++t) {
+      next_stage(t);
+#pragma unroll
+      for (int h = 0; h < kDepth / 16; ++h) {
+        Pieces s;
+        read(s, t, h);
+        multiply(s);
+      }
+    }
+  }
+
+  // A wave's sums to write: its own, or the block of its number, of all waves.
+  float16v sum[kOi][kOj];
+  const int oi = Tile_::waves_k > 1 ? wave / 2 * 32 : wi, oj = Tile_::waves_k > 1 ? wave % 2 * 32 : wj;
+  if constexpr (Tile_::waves_k == 1) {
+#pragma unroll
+    for (int x = 0; x < kOi; ++x)
+#pragma unroll
+      for (int y = 0; y < kOj; ++y) sum[x][y] = acc[x][y];
+  } else {
+    float4* part = reinterpret_cast<float4*>(lds);  // [waves][4 blocks][4][64 lanes]
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float16v& v = acc[k >> 1][k & 1];
+        part[((wave * 4 + k) * 4 + e) * 64 + lane] = make_float4(v[e * 4], v[e * 4 + 1], v[e * 4 + 2], v[e * 4 + 3]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float4 t = part[(wave * 4 + e) * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const float4 v = part[((w * 4 + wave) * 4 + e) * 64 + lane];
+        t.x += v.x;
+        t.y += v.y;
+        t.z += v.z;
+        t.w += v.w;
+      }
+      sum[0][0][e * 4] = t.x;
+      sum[0][0][e * 4 + 1] = t.y;
+      sum[0][0][e * 4 + 2] = t.z;
+      sum[0][0][e * 4 + 3] = t.w;
     }
   }
 
@@ -274,17 +387,18 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
   const _Float16* add = kStep == kSquareX ? nullptr : a.add.p + blockIdx.z * a.add.batch;
   _Float16* out = kStep == kApplyLast ? nullptr : a.out.p + blockIdx.z * a.out.batch;
 #pragma unroll
-  for (int x = 0; x < kBlocks; ++x)
+  for (int x = 0; x < kOi; ++x)
 #pragma unroll
-    for (int y = 0; y < kBlocks; ++y)
+    for (int y = 0; y < kOj; ++y)
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
-        const int i = bi * kTile + wi + x * 32 + f * 8 + (lane >> 5) * 4;
-        const int j = bj * kTile + wj + y * 32 + (lane & 31);
+        const int i = bi * kTile + oi + x * 32 + f * 8 + (lane >> 5) * 4;
+        const int j = bj * kTile + oj + y * 32 + (lane & 31);
+        if (i >= rows_i || j >= rows_j) continue;
         float v[4];
         if constexpr (kStep == kSquareX) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = acc[x][y][f * 4 + e] * 0x1p-15f;
+          for (int e = 0; e < 4; ++e) v[e] = sum[x][y][f * 4 + e] * 0x1p-15f;
         } else {
           const int64_t at = (int64_t)j * a.add.ld + i;
           const half4 hi = *reinterpret_cast<const half4*>(add + at);
@@ -293,8 +407,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(ProdArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float old = (float)hi[e] + (float)lo[e];
-            v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, acc[x][y][f * 4 + e], kB * 0.5f * old)
-                                     : __builtin_fmaf(0x1p-14f, acc[x][y][f * 4 + e], kA * old);
+            v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, sum[x][y][f * 4 + e], kB * 0.5f * old)
+                                     : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], kA * old);
           }
         }
         if constexpr (kStep == kApplyLast) {
@@ -590,21 +704,18 @@ __global__ __launch_bounds__(kPanelThreads) void k_orth_panel(User u, PanelWork 
 
 struct Layout {
   Shape s;
-  int tile;
   int64_t xs, as;  // elements of a plane of X and of A
   int64_t sums, bytes;  // offset of the sums of squares; all
   int nsums;            // of a matrix
   int panels;           // of a matrix of few rows, or 0
 };
 
-// Tiles of 128 unless they are fewer than the device's units.
 Layout layout(int64_t batch, int64_t rows, int64_t cols) {
-  Layout l;
+  Layout l{};
   l.s.turned = rows > cols;
   l.s.m = (int)std::min(rows, cols);
   l.s.n = (int)std::max(rows, cols);
   const auto up = [](int64_t v, int64_t t) { return (v + t - 1) / t * t; };
-  const int64_t t128 = up(l.s.m, 128) / 128;
   l.nsums = (int)std::min<int64_t>((rows + 3) / 4, kNormBlocks);
   // (as many bytes for a matrix as for its transpose)
   const int64_t sums = batch * std::min<int64_t>((l.s.n + 3) / 4, kNormBlocks) * (int64_t)sizeof(double);
@@ -614,51 +725,105 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
     l.bytes = l.panels == 1 ? 0 : l.sums + sums;
     return l;
   }
-  l.tile = batch * t128 * (t128 + 1) / 2 >= 256 ? 128 : 64;
-  l.s.mp = (int)up(l.s.m, l.tile);
-  l.s.np = (int)up(l.s.n, l.tile);
+  l.s.mp = (int)up(l.s.m, kPad);
+  l.s.np = (int)up(l.s.n, kPad);
   l.xs = (int64_t)l.s.mp * l.s.np;
   l.as = (int64_t)l.s.mp * l.s.mp;
   // X, two of X^T, A and B, two planes each
-  l.sums = batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16);
-  l.sums = up(l.sums, 256);
+  l.sums = up(batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16), 256);
   l.bytes = l.sums + sums;
   return l;
 }
 
-template <class T, int kTile, int kPlanes, int kStep>
-hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
+using Tile64K = Tile<64, 1, 1, 4, 64, 131072>;
+using Tile64 = Tile<64, 2, 2, 1, 32, 65536>;
+using Tile128 = Tile<128, 2, 2, 1, 32, 65536>;
+using Tile192 = Tile<192, 2, 2, 1, 32, 98304>;
+using Tile256 = Tile<256, 2, 4, 1, 32, 131072>;
+
+// Which tile a product takes: that of the least time by what the kernels
+// measured, us a tile on a unit of its own, for 32 of k (pairs and single
+// halves) and beside that (results of one matrix and of X with X^T).
+//
+// Large tiles read less for a product, 4096 x 4096 B X in pairs 411 us with 256,
+// 442 with 128, 650 with 64; but tiles come in rounds of one a unit: the 253 tiles
+// of 192 of a symmetric result of 4096 take 226 us, its 136 of 256 266, its 528
+// of 128 295. At most one round of 64 and sums of kLongSum or more: four waves by
+// pieces of k (1024 x 4096 X X^T in single halves 16 us, 26 in quarters; in
+// pairs 36 and 41; sums of 300 8.1 and 6.5).
+constexpr int kLongSum = 1024;
+struct TileTime {
+  int side;
+  float depth[2], rest[2];
+};
+constexpr TileTime kTimes[] = {{64, {0.34f, 0.15f}, {2.5f, 2.7f}},
+                               {128, {0.9f, 0.4f}, {5.0f, 11.0f}},
+                               {192, {1.75f, 0.75f}, {8.0f, 20.0f}},
+                               {256, {3.2f, 1.5f}, {10.0f, 16.0f}}};
+constexpr int kUnits = 256;
+int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, int planes, bool* one_round) {
+  int best = 0;
+  float least = 0.0f;
+  for (const TileTime& t : kTimes) {
+    const int64_t ti = (a.s.mp + t.side - 1) / t.side, tj = (a.s.np + t.side - 1) / t.side;
+    const int64_t tiles = batch * (symmetric ? ti * (ti + 1) / 2 : ti * tj), rounds = (tiles + kUnits - 1) / kUnits;
+    const float time = (float)rounds * (t.depth[2 - planes] * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
+    if (best == 0 || time < least) {
+      best = t.side;
+      least = time;
+      *one_round = rounds == 1;
+    }
+  }
+  return best;
+}
+
+template <class T, class Tile_, int kPlanes, int kStep>
+hipError_t product_of(ProdArgs a, int64_t batch, hipStream_t st) {
   constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
+  a.ti = (a.s.mp + Tile_::side - 1) / Tile_::side;
+  a.tj = kSym ? a.ti : (a.s.np + Tile_::side - 1) / Tile_::side;
   const unsigned tiles = kSym ? (unsigned)(a.ti * (a.ti + 1) / 2) : (unsigned)(a.ti * a.tj);
-  hipLaunchKernelGGL((k_orth_product<T, kTile, kPlanes, kStep>), dim3(tiles, 1, (unsigned)batch), dim3(kThreads), 0, st, a);
+  const hipError_t e = allow_lds<k_orth_product<T, Tile_, kPlanes, kStep>>(Tile_::lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_orth_product<T, Tile_, kPlanes, kStep>), dim3(tiles, 1, (unsigned)batch),
+                     dim3(64 * Tile_::waves), Tile_::lds, st, a);
   return hipGetLastError();
 }
 
-template <class T, int kTile, int kPlanes>
-hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, char* work, hipStream_t st, Planes X,
-                   Planes XT0, Planes XT1, Planes A, Planes B) {
+template <class T, int kPlanes, int kStep>
+hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
+  bool one_round = false;
+  const int side = tile_side(a, batch, kStep == kSquareX || kStep == kSquareA, kPlanes, &one_round);
+  if (side == 64 && one_round && a.k >= kLongSum) return product_of<T, Tile64K, kPlanes, kStep>(a, batch, st);
+  if (side == 64) return product_of<T, Tile64, kPlanes, kStep>(a, batch, st);
+  if (side == 128) return product_of<T, Tile128, kPlanes, kStep>(a, batch, st);
+  if (side == 192) return product_of<T, Tile192, kPlanes, kStep>(a, batch, st);
+  return product_of<T, Tile256, kPlanes, kStep>(a, batch, st);
+}
+
+template <class T, int kPlanes>
+hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, hipStream_t st, Planes X, Planes XT0,
+                   Planes XT1, Planes A, Planes B) {
   Planes now = XT0, next = XT1;
   for (int k = 0; k < steps; ++k) {
     const bool last = k + 1 == steps;
     ProdArgs a{};
     a.s = l.s;
     a.u = u;
-    a.ti = a.tj = l.s.mp / kTile;
     a.P = a.Q = X;
     a.out = A;
     a.k = l.s.np;
-    hipError_t e = product<float, kTile, kPlanes, kSquareX>(a, batch, st);
+    hipError_t e = product<float, kPlanes, kSquareX>(a, batch, st);
     if (e != hipSuccess) return e;
     a.P = a.Q = a.add = A;
     a.out = B;
     a.k = l.s.mp;
-    if ((e = product<float, kTile, kPlanes, kSquareA>(a, batch, st)) != hipSuccess) return e;
+    if ((e = product<float, kPlanes, kSquareA>(a, batch, st)) != hipSuccess) return e;
     a.P = B;
     a.Q = a.add = now;
     a.out = next;
     a.out2 = X;
-    a.tj = l.s.np / kTile;
-    e = last ? product<T, kTile, kPlanes, kApplyLast>(a, batch, st) : product<float, kTile, kPlanes, kApplyB>(a, batch, st);
+    e = last ? product<T, kPlanes, kApplyLast>(a, batch, st) : product<float, kPlanes, kApplyB>(a, batch, st);
     if (e != hipSuccess) return e;
     std::swap(now, next);
   }
@@ -713,16 +878,12 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int pr = l.s.turned ? l.s.np : l.s.mp, pc = l.s.turned ? l.s.mp : l.s.np;  // G's sides, padded
-  hipLaunchKernelGGL((k_orth_begin<T>), dim3(pc / 64, pr / 64, (unsigned)batch), dim3(kThreads), 0, st, u, l.s, sums,
+  hipLaunchKernelGGL((k_orth_begin<T>), dim3((unsigned)(cols + 63) / 64, (unsigned)(rows + 63) / 64, (unsigned)batch), dim3(kThreads), 0, st, u, l.s, sums,
                      l.nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0, (int)rows, (int)cols);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if constexpr (std::is_same<T, bf16>::value)
-    if (l.s.m > kSmall)
-      return l.tile == 128 ? iterate<T, 128, 1>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
-                           : iterate<T, 64, 1>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
-  return l.tile == 128 ? iterate<T, 128, 2>(l, u, batch, steps, work, st, X, XT0, XT1, A, B)
-                       : iterate<T, 64, 2>(l, u, batch, steps, work, st, X, XT0, XT1, A, B);
+    if (l.s.m > kSmall) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B);
+  return iterate<T, 2>(l, u, batch, steps, st, X, XT0, XT1, A, B);
 }
 
 int check_sizes(int64_t batch, int64_t rows, int64_t cols) {
