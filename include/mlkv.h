@@ -300,7 +300,8 @@ int mlkv_read_staleness(mlkv_table *t, const int64_t *d_rows, int64_t n, uint32_
  * Rows lie `*_stride` ELEMENTS apart (>= the row's length, or 0 in an input
  * whose rows are all the same; any alignment of the element type), the elements of a
  * row next to each other. Arguments are checked before anything is launched:
- * MLKV_EINVAL leaves every buffer as it was. Equal calls give equal bits. */
+ * MLKV_EINVAL leaves every buffer as it was. Equal calls on equal data, at
+ * addresses that are equal modulo 16 bytes, give equal bits. */
 
 /* Element types of the calls below. */
 enum { MLKV_F32 = 0, MLKV_BF16 = 1, MLKV_F16 = 2 };
@@ -378,11 +379,14 @@ int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_t
  *     X = G / (||G|| + eps)     (Frobenius norm; transposed where rows > cols)
  *     `steps` times:  A = X X^T,  B = b A + c A^2,  X = a X + B X
  *     out = X                   (transposed back)
- * with (a, b, c) = (3.4445, -4.7750, 2.0315). The norm is summed in fp64; X, A
+ * with (a, b, c) = (3.4445, -4.7750, 2.0315). The norm is summed in fp64. X, A
  * and B are held as pairs of fp16 numbers (22 bits of an element, but none
  * below 2^-40, so that an update whose norm is far below eps loses digits) and
- * their products are summed in fp32. G and out are of type dtype, row-major with rows *_stride
- * and matrices *_batch_stride elements apart; out may be G itself (same strides).
+ * their products are summed in fp32; for bf16 updates of more than 128 rows and
+ * columns A, B and the products' operands are single fp16 numbers, 11 bits, which
+ * leaves an error below bf16's own rounding. G and out are of type dtype, row-major
+ * with rows *_row_stride and matrices *_batch_stride elements apart; out may be
+ * G itself (same strides).
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.
  * 0 <= batch <= 65535, 1 <= rows, cols <= MLKV_ORTH_MAX_DIM, 1 <= steps <= 64,
  * eps > 0 and finite.

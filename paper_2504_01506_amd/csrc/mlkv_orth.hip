@@ -383,35 +383,67 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
   }
 
   // Epilogue. A lane holds column j = lane % 32 of each block, rows i in fours.
+  // Blocks go to and from memory through LDS, a wave's own 5 KB, as rows of 64
+  // bytes in 16-byte pieces: written straight from these registers a row is
+  // four pieces of 16 bytes, or its other side 2 bytes a lane (1024 x 4096 B X in
+  // single halves 23.8 us, 28.0 straight; 4096 x 4096 in pairs 384 and 411).
   constexpr bool kPairIn = kPlanes == 2 || !kSym, kPairOut = kPlanes == 2 || kStep == kApplyB;
-  const _Float16* add = kStep == kSquareX ? nullptr : a.add.p + blockIdx.z * a.add.batch;
-  _Float16* out = kStep == kApplyLast ? nullptr : a.out.p + blockIdx.z * a.out.batch;
+  constexpr int kRow = 40;  // halves of a row there: 16 bytes more than it holds, against bank conflicts
+  __syncthreads();
+  _Float16* mine = lds + wave * (2 * 32 * kRow);
+  // the block's rows of a plane from LDS, or to it; `from` and `to` point at the block's corner
+  const auto store_block = [&](const _Float16* from, _Float16* to, int ld) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = (lane + 64 * k) >> 2, c = lane & 3;
+      *reinterpret_cast<half8*>(to + (int64_t)r * ld + c * 8) = *reinterpret_cast<const half8*>(from + r * kRow + c * 8);
+    }
+  };
+  const auto load_block = [&](const _Float16* from, int ld, _Float16* to) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = (lane + 64 * k) >> 2, c = lane & 3;
+      *reinterpret_cast<half8*>(to + r * kRow + c * 8) = *reinterpret_cast<const half8*>(from + (int64_t)r * ld + c * 8);
+    }
+  };
+  const auto wave_sync = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
 #pragma unroll
   for (int x = 0; x < kOi; ++x)
 #pragma unroll
-    for (int y = 0; y < kOj; ++y)
+    for (int y = 0; y < kOj; ++y) {
+      const int i0 = bi * kTile + oi + x * 32, j0 = bj * kTile + oj + y * 32;
+      if (i0 >= rows_i || j0 >= rows_j) continue;  // (sides are padded to whole blocks)
+      const int il = (lane >> 5) * 4, jl = lane & 31;
+      if constexpr (kStep != kSquareX) {
+        const _Float16* add = a.add.p + blockIdx.z * a.add.batch + (int64_t)j0 * a.add.ld + i0;
+        load_block(add, a.add.ld, mine);
+        if constexpr (kPairIn) load_block(add + a.add.plane, a.add.ld, mine + 32 * kRow);
+        wave_sync();
+      }
+      half4 hi[4], lo[4];
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
-        const int i = bi * kTile + oi + x * 32 + f * 8 + (lane >> 5) * 4;
-        const int j = bj * kTile + oj + y * 32 + (lane & 31);
-        if (i >= rows_i || j >= rows_j) continue;
         float v[4];
         if constexpr (kStep == kSquareX) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = sum[x][y][f * 4 + e] * 0x1p-15f;
         } else {
-          const int64_t at = (int64_t)j * a.add.ld + i;
-          const half4 hi = *reinterpret_cast<const half4*>(add + at);
-          half4 lo = {};
-          if constexpr (kPairIn) lo = *reinterpret_cast<const half4*>(add + a.add.plane + at);
+          const half4 h = *reinterpret_cast<const half4*>(mine + jl * kRow + f * 8 + il);
+          half4 l = {};
+          if constexpr (kPairIn) l = *reinterpret_cast<const half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float old = (float)hi[e] + (float)lo[e];
+            const float old = (float)h[e] + (float)l[e];
             v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, sum[x][y][f * 4 + e], kB * 0.5f * old)
                                      : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], kA * old);
           }
         }
         if constexpr (kStep == kApplyLast) {
+          const int i = i0 + f * 8 + il, j = j0 + jl;
           T* to = static_cast<T*>(a.u.out) + blockIdx.z * a.u.o_batch;
           if (j < a.s.n) {
 #pragma unroll
@@ -420,29 +452,45 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
                 to[a.s.turned ? j * a.u.o_row + i + e : (i + e) * a.u.o_row + j] = (T)(v[e] * 0x1p-15f);
           }
         } else {
-          half4 hi, lo;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             _Float16 h, l;
             split(v[e], h, l);
-            hi[e] = h;
-            lo[e] = l;
-          }
-          const int64_t at = (int64_t)j * a.out.ld + i;
-          *reinterpret_cast<half4*>(out + at) = hi;
-          if constexpr (kPairOut) *reinterpret_cast<half4*>(out + a.out.plane + at) = lo;
-          if (kStep == kApplyB || (kSym && bi != bj)) {
-            const Planes& o = kSym ? a.out : a.out2;
-            _Float16* to = o.p + blockIdx.z * o.batch;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int64_t to_at = (int64_t)(i + e) * o.ld + j;
-              to[to_at] = hi[e];
-              if constexpr (kPlanes == 2) to[o.plane + to_at] = lo[e];  // (of X only the products read this one)
-            }
+            hi[f][e] = h;
+            lo[f][e] = l;
           }
         }
       }
+      wave_sync();
+      if constexpr (kStep != kApplyLast) {
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          *reinterpret_cast<half4*>(mine + jl * kRow + f * 8 + il) = hi[f];
+          if constexpr (kPairOut) *reinterpret_cast<half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il) = lo[f];
+        }
+        wave_sync();
+        _Float16* out = a.out.p + blockIdx.z * a.out.batch + (int64_t)j0 * a.out.ld + i0;
+        store_block(mine, out, a.out.ld);
+        if constexpr (kPairOut) store_block(mine + 32 * kRow, out + a.out.plane, a.out.ld);
+        wave_sync();
+        if (kStep == kApplyB || (kSym && bi != bj)) {
+          const Planes& o = kSym ? a.out : a.out2;
+#pragma unroll
+          for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              mine[(f * 8 + il + e) * kRow + jl] = hi[f][e];
+              // (X's lo is not read by products of single halves)
+              if constexpr (kPlanes == 2) mine[(32 + f * 8 + il + e) * kRow + jl] = lo[f][e];
+            }
+          wave_sync();
+          _Float16* to = o.p + blockIdx.z * o.batch + (int64_t)i0 * o.ld + j0;
+          store_block(mine, to, o.ld);
+          if constexpr (kPlanes == 2) store_block(mine + 32 * kRow, to + o.plane, o.ld);
+          wave_sync();
+        }
+      }
+    }
 }
 
 // ---- matrices of few rows: panels in LDS ----
@@ -741,9 +789,9 @@ using Tile128 = Tile<128, 2, 2, 1, 32, 65536>;
 using Tile192 = Tile<192, 2, 2, 1, 32, 98304>;
 using Tile256 = Tile<256, 2, 4, 1, 32, 131072>;
 
-// Which tile a product takes: that of the least time by what the kernels
-// measured, us a tile on a unit of its own, for 32 of k (pairs and single
-// halves) and beside that (results of one matrix and of X with X^T).
+// Which tile a product takes: that of the least time by a fit to what the
+// kernels measured, us a tile on a unit of its own, for 32 of k (pairs and
+// single halves) and beside that (symmetric results, and X with X^T).
 //
 // Large tiles read less for a product, 4096 x 4096 B X in pairs 411 us with 256,
 // 442 with 128, 650 with 64; but tiles come in rounds of one a unit: the 253 tiles
@@ -928,7 +976,8 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
   const Layout l = layout(batch, rows, cols);
   if (l.bytes > 0 && (d_work == nullptr || work_bytes < l.bytes))
     return op_error(MLKV_EINVAL, "work is smaller than mlkv_orthogonalize_workspace");
-  if (!all_aligned(256, 1, {d_work}, {})) return op_error(MLKV_EINVAL, "work must be at a multiple of 256 bytes");
+  if (l.bytes > 0 && !all_aligned(256, 1, {d_work}, {}))
+    return op_error(MLKV_EINVAL, "work must be at a multiple of 256 bytes");
   User u;
   u.g = d_g;
   u.out = d_out;
