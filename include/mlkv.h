@@ -385,7 +385,7 @@ int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_t
  * their products are summed in fp32; for bf16 updates of more than 128 rows and
  * columns A, B and the products' operands are single fp16 numbers, 11 bits, which
  * leaves an error below bf16's own rounding. G and out are of type dtype, row-major
- * with rows *_row_stride and matrices *_batch_stride elements apart; out may be
+ * with rows (out_)row_stride and matrices (out_)batch_stride elements apart; out may be
  * G itself (same strides).
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.
  * 0 <= batch <= 65535, 1 <= rows, cols <= MLKV_ORTH_MAX_DIM, 1 <= steps <= 64,

@@ -7,7 +7,8 @@ gradients), and the update of a dense weight that no table holds
 computes): tensors are checked here and passed as device pointers, outputs and
 workspaces that are not given are allocated by torch, and the work is queued on
 `stream` (the current stream of the tensors' device unless given) without
-waiting for it. There is no fallback: without the built library, or on tensors
+waiting for it. They stand outside torch's autograd: gradients are calls of
+their own. There is no fallback: without the built library, or on tensors
 that are not on a GPU, a call raises.
 
 As with any torch call on a side stream, a tensor that is given and was made on
@@ -27,6 +28,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 _TYPES = {torch.float32: mlkv.MLKV_F32, torch.bfloat16: mlkv.MLKV_BF16, torch.float16: mlkv.MLKV_F16}
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -148,7 +153,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     with _Queue(x, stream) as st:
         out = _out(out, "out", x)
         ostep = _rows(out, "out")[2]
-        mlkv._check(mlkv.mlkv_layer_norm(x, step, weight, bias, n, dim, eps, kind, wkind, out, ostep, st))
+        mlkv._check(mlkv.load().mlkv_layer_norm(x.data_ptr(), step, _ptr(weight), _ptr(bias), n, dim, eps, kind, wkind,
+                                                out.data_ptr(), ostep, st))
     return out
 
 
@@ -170,10 +176,12 @@ def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch
         ostep = _rows(out, "out")[2]
         dw = x.new_empty(dim) if weight is None else torch.empty_like(weight)
         db = torch.empty_like(dw)
-        nbytes = _bytes(mlkv.mlkv_layer_norm_grad_workspace(n, dim))
+        lib = mlkv.load()
+        nbytes = _bytes(lib.mlkv_layer_norm_grad_workspace(n, dim))
         work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-        mlkv._check(mlkv.mlkv_layer_norm_grad(x, step, weight, grad, gstep, n, dim, eps, kind, wkind, out, ostep, dw,
-                                              db, work, nbytes, st))
+        mlkv._check(lib.mlkv_layer_norm_grad(x.data_ptr(), step, _ptr(weight), grad.data_ptr(), gstep, n, dim, eps, kind,
+                                             wkind, out.data_ptr(), ostep, dw.data_ptr(), db.data_ptr(),
+                                             work.data_ptr(), nbytes, st))
     return out, dw, db
 
 
@@ -196,14 +204,16 @@ def log_probs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, stream=N
     _check(tokens, "tokens", logits, torch.int64, lead, dense=True)
     top = int(top)
     with _Queue(logits, stream) as st:
-        nbytes = _bytes(mlkv.mlkv_log_probs_workspace(n, vocab, top, kind))
+        lib = mlkv.load()
+        nbytes = _bytes(lib.mlkv_log_probs_workspace(n, vocab, top, kind))
 
         logp = torch.empty(lead, dtype=torch.float32, device=logits.device)
         r = LogProbs(logp, torch.empty_like(logp), logp.new_empty((*lead, 2)),
                      tokens.new_empty((*lead, top)) if top else None, logp.new_empty((*lead, top)) if top else None)
         work = torch.empty(nbytes, dtype=torch.uint8, device=logits.device) if nbytes else None
-        mlkv._check(mlkv.mlkv_log_probs(logits, step, tokens, n, vocab, top, kind, r.logp, r.entropy, r.stats,
-                                        r.top_ids, r.top_logp, work, nbytes, st))
+        mlkv._check(lib.mlkv_log_probs(logits.data_ptr(), step, tokens.data_ptr(), n, vocab, top, kind, logp.data_ptr(),
+                                       r.entropy.data_ptr(), r.stats.data_ptr(), _ptr(r.top_ids), _ptr(r.top_logp),
+                                       _ptr(work), nbytes, st))
     return r
 
 
@@ -233,8 +243,9 @@ def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: 
     with _Queue(logits, stream) as st:
         out = _out(out, "out", logits)
         ostep = _rows(out, "out")[2]
-        mlkv._check(mlkv.mlkv_log_probs_grad(logits, step, tokens, stats, entropy, logp_grad, entropy_grad, n, vocab,
-                                             kind, out, ostep, st))
+        mlkv._check(mlkv.load().mlkv_log_probs_grad(logits.data_ptr(), step, _ptr(tokens), stats.data_ptr(),
+                                                    _ptr(entropy), _ptr(logp_grad), _ptr(entropy_grad), n, vocab, kind,
+                                                    out.data_ptr(), ostep, st))
     return out
 
 
@@ -268,8 +279,9 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
     with _Queue(g, stream) as st:
         out = _out(out, "out", g)
         ob, orow = _matrices(out, "out")
-        nbytes = _bytes(mlkv.mlkv_orthogonalize_workspace(batch, rows, cols))
+        lib = mlkv.load()
+        nbytes = _bytes(lib.mlkv_orthogonalize_workspace(batch, rows, cols))
         work = torch.empty(nbytes, dtype=torch.uint8, device=g.device) if nbytes else None
-        mlkv._check(mlkv.mlkv_orthogonalize(g, gb, gr, batch, rows, cols, int(steps), eps, kind, out, ob, orow, work,
-                                            nbytes, st))
+        mlkv._check(lib.mlkv_orthogonalize(g.data_ptr(), gb, gr, batch, rows, cols, int(steps), eps, kind,
+                                           out.data_ptr(), ob, orow, _ptr(work), nbytes, st))
     return out

@@ -296,6 +296,26 @@ def test_gradient_against_differences(gen):
 
 
 @pytest.mark.gpu
+def test_offsets_past_32_bits(gen):
+    from paper_2504_01506_amd import ops
+    n, vocab = 40_000, 120_001          # 4.8e9 logits
+    few = logits(gen, 100, vocab, torch.bfloat16)
+    x = few.repeat(n // 100, 1)
+    t = some_tokens(gen, 100, vocab).repeat(n // 100)
+    r = ops.log_probs(x, t, top=4)
+    check(x[-3:], t[-3:], 4)
+    want = reference(few, t[:100], 4)
+    assert torch.equal(r.top_ids, want[4].repeat(n // 100, 1))
+    assert (r.logp.double() - want[0].repeat(n // 100)).abs().max() <= 1e-4
+    one = torch.ones(n, device="cuda")
+    first = ops.log_probs_grad(x[:100], t[:100], r.stats[:100], None, one[:100])
+    ops.log_probs_grad(x, t, r.stats, None, one, out=x)
+    for at in (n - 200, n // 200 * 100):
+        # rows at one place modulo 16 bytes are cut alike: 100 rows are 24,000,200 bytes, 8 modulo 16, 200 of them 0
+        assert torch.equal(x[at:at + 100], first)
+
+
+@pytest.mark.gpu
 def test_streams_and_graph_replays(gen):
     from paper_2504_01506_amd import ops
     x, x2 = logits(gen, 3, 60_000, torch.bfloat16), logits(gen, 500, 40_000, torch.bfloat16)

@@ -212,6 +212,20 @@ def test_gradient_against_differences(gen):
 
 
 @pytest.mark.gpu
+def test_offsets_past_32_bits(gen):
+    from paper_2504_01506_amd import ops
+    few, dy = rows(gen, 512, 4097, torch.float16), rows(gen, 512, 4097, torch.float16)
+    w = torch.randn(4097, generator=gen, device="cuda")
+    x, g = few.repeat(2100, 1), dy.repeat(2100, 1)      # 4.4e9 elements
+    want, want_g = ops.layer_norm(few, w), ops.layer_norm_grad(few, w, dy)[0]
+    check_forward(want, few, w, None, 1e-5)
+    out = ops.layer_norm(x, w)
+    assert torch.equal(out[-512:], want) and torch.equal(out[1050 * 512:1051 * 512], want)
+    got = ops.layer_norm_grad(x, w, g, out=out)[0]
+    assert torch.equal(got[-512:], want_g) and torch.equal(got[1050 * 512:1051 * 512], want_g)
+
+
+@pytest.mark.gpu
 def test_streams_and_graph_replays(gen):
     from paper_2504_01506_amd import ops
     x, dy = rows(gen, 3000, 256, torch.bfloat16), rows(gen, 3000, 256, torch.bfloat16)
