@@ -630,7 +630,7 @@ struct GradArgs {
   const float* g_logp;     // or NULL
   const float* g_entropy;  // or NULL
   void* out;
-  int64_t stride, out_stride;
+  int64_t stride, out_stride, n;
   int vocab, chunks;
 };
 
@@ -653,20 +653,23 @@ __device__ __forceinline__ float grad_of(float x, int i, const RowGrad& g) {
   return g.none ? 0.0f : d;
 }
 
-template <class T, bool kEntropy>
+// kTeam threads take a chunk of a row: a block, or a wave where that is all of it.
+template <class T, bool kEntropy, int kTeam>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
   constexpr int V = 16 / sizeof(T);
-  const int64_t row = blockIdx.x / (uint32_t)a.chunks;
-  const int chunk = (int)(blockIdx.x % (uint32_t)a.chunks);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x % kTeam;
+  const int64_t row = kTeam == 64 ? (int64_t)blockIdx.x * (kChunkThreads / 64) + threadIdx.x / 64
+                                  : blockIdx.x / (uint32_t)a.chunks;
+  const int chunk = kTeam == 64 ? 0 : (int)(blockIdx.x % (uint32_t)a.chunks);
+  if (row >= a.n) return;
   const T* x = static_cast<const T*>(a.logits) + row * a.stride;
   T* out = static_cast<T*>(a.out) + row * a.out_stride;
   const Cut<T> cut(x, a.vocab);
-  const int first = chunk * kGradVecs * kChunkThreads + tid;
+  const int first = chunk * kGradVecs * kTeam + tid;
   Raw p[kGradVecs] = {};
 #pragma unroll
   for (int j = 0; j < kGradVecs; ++j) {
-    const int v = first + j * kChunkThreads;
+    const int v = first + j * kTeam;
     if (v < cut.vecs) p[j] = load_raw(x + cut.head + (int64_t)v * V);
   }
   int extra = -1;
@@ -696,7 +699,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
   }
 #pragma unroll
   for (int j = 0; j < kGradVecs; ++j) {
-    const int v = first + j * kChunkThreads;
+    const int v = first + j * kTeam;
     if (v < cut.vecs) {
       const int i = cut.head + v * V;
       LoosePack<T, V> o;
@@ -790,22 +793,27 @@ hipError_t launch_logp(LogpArgs a, const ChunkPlan& c, hipStream_t st) {
 }
 
 template <class T>
-hipError_t launch_logp_grad(GradArgs a, int64_t n, hipStream_t st) {
-  const int64_t slice = std::max<int64_t>(1, kGridBlocks / a.chunks);
+hipError_t launch_logp_grad(GradArgs a, bool wave, hipStream_t st) {
+  const int64_t slice = std::max<int64_t>(1, kGridBlocks / a.chunks), n = a.n;
   for (int64_t at = 0; at < n; at += slice) {
-    const int64_t rows = std::min(slice, n - at);
-    const dim3 grid((unsigned)(rows * a.chunks)), block(kChunkThreads);
-    if (a.g_entropy != nullptr) hipLaunchKernelGGL((k_logp_grad<T, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_logp_grad<T, false>), grid, block, 0, st, a);
+    a.n = std::min(slice, n - at);
+    const dim3 grid((unsigned)(wave ? (a.n + 3) / 4 : a.n * a.chunks)), block(kChunkThreads);
+    if (wave) {
+      if (a.g_entropy != nullptr) hipLaunchKernelGGL((k_logp_grad<T, true, 64>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((k_logp_grad<T, false, 64>), grid, block, 0, st, a);
+    } else {
+      if (a.g_entropy != nullptr) hipLaunchKernelGGL((k_logp_grad<T, true, kChunkThreads>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((k_logp_grad<T, false, kChunkThreads>), grid, block, 0, st, a);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    a.logits = static_cast<const T*>(a.logits) + rows * a.stride;
-    a.out = static_cast<T*>(a.out) + rows * a.out_stride;
-    a.stats += 2 * rows;
-    if (a.tokens != nullptr) a.tokens += rows;
-    if (a.entropy != nullptr) a.entropy += rows;
-    if (a.g_logp != nullptr) a.g_logp += rows;
-    if (a.g_entropy != nullptr) a.g_entropy += rows;
+    a.logits = static_cast<const T*>(a.logits) + a.n * a.stride;
+    a.out = static_cast<T*>(a.out) + a.n * a.out_stride;
+    a.stats += 2 * a.n;
+    if (a.tokens != nullptr) a.tokens += a.n;
+    if (a.entropy != nullptr) a.entropy += a.n;
+    if (a.g_logp != nullptr) a.g_logp += a.n;
+    if (a.g_entropy != nullptr) a.g_entropy += a.n;
   }
   return hipSuccess;
 }
@@ -914,10 +922,12 @@ int mlkv_log_probs_grad(const void* d_logits, int64_t stride, const int64_t* d_t
   a.stride = stride;
   a.out_stride = grad_stride;
   a.vocab = (int)vocab;
+  a.n = n;
   const int64_t per = (int64_t)kGradVecs * kChunkThreads, vecs = vocab / (16 / size);
+  const bool wave = vecs <= kGradVecs * 64;
   a.chunks = (int)std::max<int64_t>(1, (vecs + per - 1) / per);
   const hipError_t e = dispatch_type(dtype, [&](auto t) {
-    return launch_logp_grad<decltype(t)>(a, n, static_cast<hipStream_t>(hip_stream));
+    return launch_logp_grad<decltype(t)>(a, wave, static_cast<hipStream_t>(hip_stream));
   });
   return e == hipSuccess ? MLKV_OK : op_launch_error(e, "mlkv_log_probs_grad launch");
 }

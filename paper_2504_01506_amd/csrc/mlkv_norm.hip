@@ -115,20 +115,38 @@ __device__ __forceinline__ void store_row(T* row, int c, int dim, const LoosePac
   }
 }
 
-// One thread's columns of weight or bias; `none` in those that are not its own.
+// One thread's columns of weight or bias.
 template <class T, int I, bool kFull, bool kShort>
 __device__ __forceinline__ void load_params(float (&w)[I * (16 / sizeof(T))], const void* p, bool wide, float none,
                                             const Columns<T, I, kFull>& cols, int dim) {
   constexpr int V = 16 / sizeof(T);
+  const auto take = [&](auto of) {
+    using P = decltype(of);
+    constexpr int kPer = 16 / sizeof(P);
 #pragma unroll
-  for (int i = 0; i < I; ++i)
+    for (int i = 0; i < I; ++i) {
+      const P* at = static_cast<const P*>(p) + cols.at[i];
+      if constexpr (kShort) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = cols.at[i] + j;
-      w[i * V + j] = none;
-      if (p != nullptr && (!kShort || c < dim))
-        w[i * V + j] = wide ? static_cast<const float*>(p)[c] : (float)static_cast<const T*>(p)[c];
+        for (int j = 0; j < V; ++j) w[j] = j < dim ? (float)at[j] : none;
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; j += kPer) {
+          const Raw r = load_raw(at + j);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) w[i * V + j + e] = element<P>(r, e);
+        }
+      }
     }
+  };
+  if (p == nullptr) {
+#pragma unroll
+    for (int e = 0; e < I * V; ++e) w[e] = none;
+  } else if (wide) {
+    take(float{});
+  } else {
+    take(T{});
+  }
 }
 
 // kMost: threads of a block at most, 0 for rows within waves
