@@ -368,8 +368,10 @@ int mlkv_log_probs(const void *d_logits, int64_t stride, const int64_t *d_tokens
  *     d_logits_grad[j] = a * ((j == token) - p[j]) - b * p[j] * (log p[j] + H)
  * where p comes from d_stats as mlkv_log_probs wrote it. d_logp_grad (with
  * d_tokens) or d_entropy_grad (with d_entropy) may be NULL (0). A row without a
- * distribution gets zeros, a token >= vocab NaN. d_logits_grad is of the
- * logits' type and may be d_logits (same stride). Limits as mlkv_log_probs. */
+ * distribution gets zeros, a token >= vocab NaN; with d_logp_grad, a row whose
+ * token is < 0 and whose b is 0 gets zeros whatever its logits are (a padded
+ * position's may be NaN). d_logits_grad is of the logits' type and may be
+ * d_logits (same stride). Limits as mlkv_log_probs. */
 int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_tokens, const float *d_stats,
                         const float *d_entropy, const float *d_logp_grad, const float *d_entropy_grad, int64_t n,
                         int64_t vocab, int dtype, void *d_logits_grad, int64_t grad_stride, void *hip_stream);

@@ -640,7 +640,7 @@ constexpr int kGradVecs = 4;  // vectors of a thread
 struct RowGrad {
   float m, logs, ent, a, b;
   int token;  // or -1
-  bool none;
+  bool none;  // zeros
 };
 template <bool kEntropy>
 __device__ __forceinline__ float grad_of(float x, int i, const RowGrad& g) {
@@ -682,20 +682,21 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
   g.m = a.stats[2 * row];
   g.logs = a.stats[2 * row + 1];
   g.none = g.m == -kInf;
-  g.a = 0.0f;
+  g.a = g.b = g.ent = 0.0f;
   g.token = -1;
+  if constexpr (kEntropy) {
+    g.b = a.g_entropy[row];
+    g.ent = a.entropy[row];
+  }
   if (a.g_logp != nullptr) {
     const int64_t t = a.tokens[row];
     if (t >= 0) {
       g.a = t < a.vocab ? a.g_logp[row] : __builtin_nanf("");
       g.token = t < a.vocab ? (int)t : -1;
       if (t >= a.vocab) g.none = false;
+    } else if (g.b == 0.0f) {
+      g.none = true;  // (the logits behind a batch's last position may be anything)
     }
-  }
-  g.b = g.ent = 0.0f;
-  if constexpr (kEntropy) {
-    g.b = a.g_entropy[row];
-    g.ent = a.entropy[row];
   }
 #pragma unroll
   for (int j = 0; j < kGradVecs; ++j) {

@@ -971,9 +971,9 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
   if (d_g == nullptr || d_out == nullptr) return op_error(MLKV_EINVAL, "g or out is NULL");
   if (!all_aligned(size, size, {d_g, d_out}, {}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
-  const int64_t span = (rows - 1) * out_row_stride + cols;
   if (!stride_ok(row_stride, rows, cols, true) || !stride_ok(out_row_stride, rows, cols, false))
     return op_error(MLKV_EINVAL, "row strides must be >= cols (or 0 in g)");
+  const int64_t span = (rows - 1) * (rows > 1 ? out_row_stride : 0) + cols;
   if (batch > 1 && (batch_stride < 0 || batch_stride > (int64_t(1) << 44) || !stride_ok(out_batch_stride, batch, span, false)))
     return op_error(MLKV_EINVAL, "batch strides must not make matrices overlap");
   if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))

@@ -109,8 +109,8 @@ class _Queue:
         s = self.stream
         if s is None:
             s = torch.cuda.current_stream(self.device)
-        elif isinstance(s, int):
-            s = torch.cuda.ExternalStream(s, device=self.device)
+        elif isinstance(s, int):  # (a handle; 0 is the device's default stream)
+            s = torch.cuda.ExternalStream(s, device=self.device) if s else torch.cuda.default_stream(self.device)
         elif s.device != self.device:
             raise ValueError(f"the stream is of {s.device}, the tensors are on {self.device}")
         self.held = torch.cuda.stream(s)

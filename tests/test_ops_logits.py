@@ -279,6 +279,30 @@ def test_gradient_under_masks(gen, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [300, 9000])
+def test_padded_positions_get_zeros(gen, vocab, kind):
+    """A position without a token passes no gradient, also where its logits are no numbers."""
+    from paper_2504_01506_amd import ops
+    x = logits(gen, 6, vocab, kind)
+    t = some_tokens(gen, 6, vocab)
+    t[:4] = -1
+    t[4:] = 7
+    x[0], x[1, 3], x[2, vocab - 1] = math.nan, math.inf, math.nan
+    r = ops.log_probs(x, t)
+    a = torch.ones(6, device="cuda")
+    b = torch.zeros(6, device="cuda")
+    a[:3] = math.nan  # (no use is made of it there)
+    for more in ((), (b,)):
+        g = ops.log_probs_grad(x, t, r.stats, r.entropy, a, *more)
+        assert (g[:4] == 0).all() and (g[4:] != 0).any(-1).all()
+    check_grad(x[3:].contiguous(), t[3:].contiguous(), a[3:].contiguous(), b[3:].contiguous())
+    b[2] = b[3] = 1.0
+    g = ops.log_probs_grad(x, t, r.stats, r.entropy, a, b)
+    assert (g[:2] == 0).all() and torch.isnan(g[2]).all() and (g[3] != 0).any()
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences(gen):
     from paper_2504_01506_amd import ops
     x, t = logits(gen, 5, 300, torch.float32), some_tokens(gen, 5, 300)

@@ -251,6 +251,19 @@ def test_streams_and_graph_replays(gen):
         torch.cuda.synchronize()
 
 
+@pytest.mark.gpu
+def test_the_default_stream_by_its_handle(gen):
+    from paper_2504_01506_amd import ops
+    x = rows(gen, 50, 64, torch.float32)
+    want = ops.layer_norm(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        default = torch.cuda.default_stream()
+        got = [ops.layer_norm(x, stream=s) for s in (0, default, default.cuda_stream)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
 # ---- refusals (no GPU needed: nothing is launched) ----
 def call(**change):
     a = dict(x=4096, xs=64, w=8192, b=8192, n=3, dim=64, eps=1e-5, dtype=mlkv.MLKV_F32, wdtype=mlkv.MLKV_F32,
