@@ -103,20 +103,37 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
   lo = (_Float16)(v - (float)hi);
 }
 
-// Planes of one matrix: hi at p, lo `plane` elements behind it.
+// Planes of one matrix: hi at p, lo `plane` elements behind it (to k_orth_begin 0: no lo).
 struct Planes {
   _Float16* p;
   int64_t plane, batch;
   int ld;
 };
 
-// X and X^T from G, 64 x 64 elements a block, the transposed ones through LDS.
+// X and X^T from G, 64 x 64 elements a block, 8 a thread at a time, the
+// transposed ones through LDS. Bound by memory: 2 or 4 bytes read and 8 written
+// an element.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const double* sums, int nsums, float eps,
-                                                         Planes straight, Planes turned, int rows, int cols) {
-  const int pr = s.turned ? s.np : s.mp, pc = s.turned ? s.mp : s.np;  // G's sides, padded
+__global__ __launch_bounds__(kThreads) void k_orth_begin(User u, const double* sums, int nsums, float eps, Planes straight,
+                                                         Planes turned, int rows, int cols) {
+  constexpr int V = 16 / sizeof(T);
   __shared__ float tile[64][65];
   __shared__ double part[kThreads / 64];
+  const T* g = static_cast<const T*>(u.g) + blockIdx.z * u.g_batch;
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const int y = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;  // (rows y and y + 32 of the tile)
+  Raw raw[2][8 / V];
+  bool whole[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = r0 + y + h * 32;
+    whole[h] = r < rows && c0 + c + 8 <= cols;
+#pragma unroll
+    for (int k = 0; k < 8 / V; ++k) {
+      raw[h][k] = Raw{0, 0, 0, 0};
+      if (whole[h]) raw[h][k] = load_raw(g + r * u.g_row + c0 + c + k * V);
+    }
+  }
   double t = 0.0;
   for (int k = threadIdx.x; k < nsums; k += kThreads) t += sums[(int64_t)blockIdx.z * nsums + k];
   for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
@@ -124,32 +141,42 @@ __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, Shape s, const 
   __syncthreads();
   t = part[0] + part[1] + part[2] + part[3];
   const double inv = 32768.0 / (sqrt(t) + (double)eps);
-  const T* g = static_cast<const T*>(u.g) + blockIdx.z * u.g_batch;
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  _Float16* a = straight.p + blockIdx.z * straight.batch;
-  for (int y = ty; y < 64; y += 4) {
-    const int r = r0 + y, c = c0 + tx;
-    const float v = r < rows && c < cols ? (float)((double)(float)g[r * u.g_row + c] * inv) : 0.0f;
-    tile[y][tx] = v;
-    _Float16 hi, lo;
-    split(v, hi, lo);
-    const int64_t at = (int64_t)r * straight.ld + c;
-    if (r < pr && c < pc) {
-      a[at] = hi;
-      a[straight.plane + at] = lo;
+  const auto store = [](const float (&v)[8], const Planes& to, _Float16* at) {
+    half8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      _Float16 h, l;
+      split(v[e], h, l);
+      hi[e] = h;
+      lo[e] = l;
     }
+    *reinterpret_cast<half8*>(at) = hi;
+    if (to.plane != 0) *reinterpret_cast<half8*>(at + to.plane) = lo;
+  };
+  // (sides are padded to whole tiles, with zeros)
+  _Float16* a = straight.p + blockIdx.z * straight.batch + (int64_t)r0 * straight.ld + c0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int in = y + h * 32, r = r0 + in;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x = element<T>(raw[h][e / V], e % V);
+      if (!whole[h] && r < rows && c0 + c + e < cols) x = (float)g[r * u.g_row + c0 + c + e];
+      v[e] = (float)((double)x * inv);
+      tile[in][c + e] = v[e];
+    }
+    store(v, straight, a + (int64_t)in * straight.ld + c);
   }
   __syncthreads();
-  _Float16* b = turned.p + blockIdx.z * turned.batch;
-  for (int y = ty; y < 64; y += 4) {
-    _Float16 hi, lo;
-    split(tile[tx][y], hi, lo);
-    const int64_t at = (int64_t)(c0 + y) * turned.ld + r0 + tx;
-    if (c0 + y < pc && r0 + tx < pr) {
-      b[at] = hi;
-      b[turned.plane + at] = lo;
-    }
+  _Float16* b = turned.p + blockIdx.z * turned.batch + (int64_t)c0 * turned.ld + r0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int in = y + h * 32;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = tile[c + e][in];
+    store(v, turned, b + (int64_t)in * turned.ld + c);
   }
 }
 
@@ -931,11 +958,15 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_orth_begin<T>), dim3((unsigned)(cols + 63) / 64, (unsigned)(rows + 63) / 64, (unsigned)batch), dim3(kThreads), 0, st, u, l.s, sums,
-                     l.nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0, (int)rows, (int)cols);
+  const bool single = std::is_same<T, bf16>::value && l.s.m > kSmall;
+  Planes first = X;
+  if (single) first.plane = 0;
+  hipLaunchKernelGGL((k_orth_begin<T>), dim3((unsigned)(cols + 63) / 64, (unsigned)(rows + 63) / 64, (unsigned)batch),
+                     dim3(kThreads), 0, st, u, sums, l.nsums, eps, l.s.turned ? XT0 : first, l.s.turned ? first : XT0,
+                     (int)rows, (int)cols);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if constexpr (std::is_same<T, bf16>::value)
-    if (l.s.m > kSmall) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B);
+    if (single) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B);
   return iterate<T, 2>(l, u, batch, steps, st, X, XT0, XT1, A, B);
 }
 

@@ -204,7 +204,8 @@ def call(**change):
     (dict(cols=32769), "rows and cols"), (dict(steps=0), "steps"), (dict(steps=65), "steps"), (dict(eps=0.0), "eps"),
     (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(dtype=3), "dtype"), (dict(g=None), "NULL"),
     (dict(out=None), "NULL"), (dict(gr=99), "row strides"), (dict(orow=0), "row strides"), (dict(gb=-1), "overlap"),
-    (dict(orow=1 << 62), "row strides"),    (dict(ob=6599), "overlap"), (dict(ob=0), "overlap"), (dict(out=4096, orow=101, ob=6666), "same strides"),
+    (dict(orow=1 << 62), "row strides"),
+    (dict(ob=6599), "overlap"), (dict(ob=0), "overlap"), (dict(out=4096, orow=101, ob=6666), "same strides"),
     (dict(work=None), "work"), (dict(bytes=1000), "work"), (dict(work=2 ** 24 + 128), "work"),
     (dict(g=4097), "aligned"), (dict(out=2 ** 20 + 2), "aligned")])
 def test_refusals(change, says):
