@@ -35,9 +35,10 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
-    return _TYPES[t.dtype]
+    return kind
 
 
 def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=None, dense=False):
@@ -88,11 +89,12 @@ def _rows(t: torch.Tensor, what: str) -> tuple[int, int, int]:
     return n, width, stride
 
 
-def _out(t: Optional[torch.Tensor], what: str, like: torch.Tensor) -> torch.Tensor:
+def _out_rows(t: Optional[torch.Tensor], like: torch.Tensor, width: int) -> tuple[torch.Tensor, int]:
+    """The output of rows like `like`'s, and the elements from row to row."""
     if t is None:
-        return torch.empty_like(like, memory_format=torch.contiguous_format)
-    _check(t, what, like, like.dtype, like.shape)
-    return t
+        return torch.empty_like(like, memory_format=torch.contiguous_format), width
+    _check(t, "out", like, like.dtype, like.shape)
+    return t, _rows(t, "out")[2]
 
 
 class _Queue:
@@ -151,8 +153,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     p = weight if weight is not None else bias
     wkind = kind if p is None else _TYPES[p.dtype]
     with _Queue(x, stream) as st:
-        out = _out(out, "out", x)
-        ostep = _rows(out, "out")[2]
+        out, ostep = _out_rows(out, x, dim)
         mlkv._check(mlkv.load().mlkv_layer_norm(x.data_ptr(), step, _ptr(weight), _ptr(bias), n, dim, eps, kind, wkind,
                                                 out.data_ptr(), ostep, st))
     return out
@@ -172,8 +173,7 @@ def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch
     _check(grad, "grad", x, x.dtype, x.shape)
     gstep = _rows(grad, "grad")[2]
     with _Queue(x, stream) as st:
-        out = _out(out, "out", x)
-        ostep = _rows(out, "out")[2]
+        out, ostep = _out_rows(out, x, dim)
         dw = x.new_empty(dim) if weight is None else torch.empty_like(weight)
         db = torch.empty_like(dw)
         lib = mlkv.load()
@@ -241,8 +241,7 @@ def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: 
     if entropy is not None:
         _check(entropy, "entropy", logits, torch.float32, lead, dense=True)
     with _Queue(logits, stream) as st:
-        out = _out(out, "out", logits)
-        ostep = _rows(out, "out")[2]
+        out, ostep = _out_rows(out, logits, vocab)
         mlkv._check(mlkv.load().mlkv_log_probs_grad(logits.data_ptr(), step, _ptr(tokens), stats.data_ptr(),
                                                     _ptr(entropy), _ptr(logp_grad), _ptr(entropy_grad), n, vocab, kind,
                                                     out.data_ptr(), ostep, st))
@@ -277,7 +276,10 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
     rows, cols = g.shape[-2:]
     gb, gr = _matrices(g, "g")
     with _Queue(g, stream) as st:
-        out = _out(out, "out", g)
+        if out is None:
+            out = torch.empty_like(g, memory_format=torch.contiguous_format)
+        else:
+            _check(out, "out", g, g.dtype, g.shape)
         ob, orow = _matrices(out, "out")
         lib = mlkv.load()
         nbytes = _bytes(lib.mlkv_orthogonalize_workspace(batch, rows, cols))
