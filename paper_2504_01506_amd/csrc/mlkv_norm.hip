@@ -218,13 +218,15 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(Nor
 
 // The gradient. After the mean one exchange gives the four sums that the rest
 // needs: of d = x - mean, d^2, g and g d. Each thread keeps the sums over rows
-// of its own columns in registers; a block joins them at its end.
+// of its own columns in registers, in fp64 where a row is shorter than a vector
+// (of a handful of sums one can come out near zero; at any width: 200,000 x 500
+// fp16 156 us, 127 in fp32); a block joins them at its end, also in fp64.
 // (whole 16-bit rows a block: four waves a SIMD, 128 registers)
 template <class T, int I, int kMost, bool kFull, bool kShort>
 __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMost && kFull ? 4 : 1) void k_layer_norm_grad(NormArgs a) {
   __shared__ float lds1[kNormMaxThreads / 64];
   __shared__ __align__(16) float lds2[4 * kNormMaxThreads / 64];
-  extern __shared__ __align__(16) float join[];  // [groups of the block][G * I * V] (not kBlock)
+  extern __shared__ __align__(16) float join[];  // [groups of the block, or its waves][G * I * V] (not kBlock)
   constexpr int V = 16 / sizeof(T);
   constexpr bool kBlock = kMost != 0, kAhead = kMost != kNormMaxThreads;
   const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1), dim = a.dim;
@@ -232,10 +234,12 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
   const float inv = 1.0f / (float)dim;
   const Columns<T, I, kFull> cols(l, G, dim);
   const auto own = [&](int i, int j) { return kShort ? j < dim : cols.own(i, j); };
-  float w[I * V], dw[I * V], db[I * V];
+  using Sum = std::conditional_t<kShort, double, float>;
+  float w[I * V];
+  Sum dw[I * V], db[I * V];
   load_params<T, I, kFull, kShort>(w, a.weight, a.wide_weight, 1.0f, cols, dim);
 #pragma unroll
-  for (int e = 0; e < I * V; ++e) dw[e] = db[e] = 0.0f;
+  for (int e = 0; e < I * V; ++e) dw[e] = db[e] = 0;
   const int sub = kBlock ? 0 : threadIdx.x / G;
   int64_t r = (int64_t)blockIdx.x * per + sub;
   const int64_t step = (int64_t)gridDim.x * per;
@@ -290,8 +294,11 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float h = (x[i * V + j] - off) * rstd, dy = element<T>(gr[i], j);
-          o.v[j] = (T)(rstd * (__builtin_fmaf(dy, w[i * V + j], -g_mean) - h * gh_mean));
-          dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
+          // (kShort: g rounded as it was for its mean, so that a row of one element gets 0)
+          const float g_over = kShort ? dy * w[i * V + j] - g_mean : __builtin_fmaf(dy, w[i * V + j], -g_mean);
+          o.v[j] = (T)(rstd * (g_over - h * gh_mean));
+          if constexpr (std::is_same<Sum, double>::value) dw[i * V + j] = __builtin_fma((double)dy, (double)h, dw[i * V + j]);
+          else dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
           db[i * V + j] += dy;
         }
         if (a.out != nullptr && (kFull || kShort || cols.skip[i] < V))
@@ -312,25 +319,37 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
         }
   } else {
     // by nominal column: vector i of lane l begins at (i G + l) V, its own elements end it
-    const int width = G * I * V;
+    const int width = G * I * V, parts = kShort ? kNormThreads / 64 : per;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       __syncthreads();
+      if constexpr (kShort) {
+        // (a lane a row: 64 for a few columns, joined by exchanges)
 #pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const float* t = (which ? db : dw) + i * V;
+        for (int e = 0; e < V; ++e) {
+          double t = which ? db[e] : dw[e];
+          for (int o = 1; o < 64; o *= 2) t += __shfl_xor(t, o);
+          if ((threadIdx.x & 63) == 0) join[threadIdx.x / 64 * V + e] = (float)t;
+        }
+      } else {
 #pragma unroll
-        for (int e = 0; e < V; e += 4)
-          *reinterpret_cast<float4*>(join + sub * width + (i * G + l) * V + e) =
-              make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+        for (int i = 0; i < I; ++i) {
+          const Sum* t = (which ? db : dw) + i * V;
+#pragma unroll
+          for (int e = 0; e < V; e += 4)
+            *reinterpret_cast<float4*>(join + sub * width + (i * G + l) * V + e) =
+                make_float4(t[e], t[e + 1], t[e + 2], t[e + 3]);
+        }
       }
       __syncthreads();
       for (int c = threadIdx.x; c < dim; c += kNormThreads) {
         // column c's place: in the last vector of the row the elements are at its end
         const int first = c / V * V, at = kFull || kShort || first + V <= dim ? c : c + V - (dim - first);
-        float t = 0.0f;
-        for (int k = 0; k < per; ++k) t += join[k * width + at];
-        mine[which * dim + c] = t;
+        double t = 0.0;
+        for (int k = 0; k < parts; k += 4)  // (a power of two from 4 on)
+          t += (double)((join[k * width + at] + join[(k + 1) * width + at]) +
+                        (join[(k + 2) * width + at] + join[(k + 3) * width + at]));
+        mine[which * dim + c] = (float)t;
       }
     }
   }

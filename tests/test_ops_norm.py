@@ -189,6 +189,25 @@ def test_no_rows_equal_rows_and_values_out_of_range(gen):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,pad", [(64, 0), (192, 3), (561_728, 25)])
+def test_rows_of_one_element(gen, n, pad):
+    """Such rows are their mean: nothing passes to x or weight. The gradients of 64 rows cancel here but for their
+    60 ones, as exactly as their sums (fp64 over a wave's rows) are whole numbers in fp32."""
+    from paper_2504_01506_amd import ops
+    x = rows(gen, n, 1, torch.float32, pad)
+    w = torch.randn(1, generator=gen, device="cuda")
+    dy = torch.ones(n // 64, 64, device="cuda")
+    dy[:, 0], dy[:, 63], dy[:, 5], dy[:, 60] = 2.0 ** 25, -2.0 ** 25, -2.0 ** 40, 2.0 ** 40
+    dx, dw, db = ops.layer_norm_grad(x, w, dy.view(n, 1))
+    assert (dx == 0).all() and dw.item() == 0 and db.item() == 60 * (n // 64)
+    dy = 0.01 * torch.randn(n, 1, generator=gen, device="cuda")
+    dx, dw, db = ops.layer_norm_grad(x, w, dy)
+    assert (dx == 0).all() and dw.item() == 0
+    # five roundings on the way, each of at most the sum of the parts' sizes
+    assert abs(db.item() - dy.double().sum().item()) <= 5 * 2.0 ** -24 * dy.double().abs().sum().item()
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences(gen):
     from paper_2504_01506_amd import ops
     for dim in (7, 64, 1500):
