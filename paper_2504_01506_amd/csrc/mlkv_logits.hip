@@ -8,12 +8,14 @@
 // chunks; where there are rows enough for the device, a block takes a row's
 // chunks in turn instead, and rows of few logits are a wave each. Bound by
 // HBM: 9 operations a logit, one of them an exponential (of the rate of four),
-// against 2 or 4 bytes.
+// against 2 or 4 bytes. 4096 rows of 128,000 bf16 logits with five alternatives
+// take 189 us, 5.5 TB/s; 8192 of 32,000 fp32 182 (5.8).
 //
 // Alternatives: a chunk leaves the largest logit of each group of 16 vectors.
 // A row's k largest logits are in the k groups whose largest are (equal ones
 // in the order of their indices, which is that of the groups), so only those
-// groups are read again, 1 of 250 for k = 4 and 128,000 logits.
+// groups are read again, 1 of 250 for k = 4 and 128,000 logits. (Candidates
+// picked by each block from its own logits: 4096 x 128,000 271 us against 190.)
 #include "mlkv_ops.h"
 
 #include <algorithm>
@@ -505,7 +507,9 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_chunk(LogpArgs a) {
   }
 }
 
-// Joins a row's chunks: a block a row.
+// Joins a row's chunks: a block a row. Bound by latency, one choice among the
+// groups and one among their logits: 8 us for one row of 128,000, of which the
+// chunks take 3.
 template <class T>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_join(LogpArgs a) {
   constexpr int kWaves = kChunkThreads / 64;
@@ -537,7 +541,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_join(LogpArgs a) {
 }
 
 // A row a block, chunk by chunk: no join, and while a block seeks its
-// alternatives the others on its unit read.
+// alternatives the others on its unit read (4096 x 128,000 bf16 with five: 189 us).
 constexpr int kRowVecs = 8, kRowGroups = 4096;  // vectors a thread and chunk; groups of a row at most
 template <class T, bool kTop>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_long(LogpArgs a) {
@@ -575,7 +579,9 @@ __global__ __launch_bounds__(kChunkThreads) void k_logp_long(LogpArgs a) {
   }
 }
 
-// Rows of at most 64 * L vectors: a wave each, four a block.
+// Rows of at most 64 * L vectors: a wave each, four a block (16,384 x 1000 bf16
+// 22 us, 43 with a block a row; 100,000 x 100 78, bound by the latency of a wave's
+// dependent steps, 234 with a block).
 template <class T, int L, bool kTop>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_rows(LogpArgs a) {
   constexpr int V = 16 / sizeof(T), kWaves = kChunkThreads / 64;
@@ -653,7 +659,9 @@ __device__ __forceinline__ float grad_of(float x, int i, const RowGrad& g) {
   return g.none ? 0.0f : d;
 }
 
-// kTeam threads take a chunk of a row: a block, or a wave where that is all of it.
+// kTeam threads take a chunk of a row: a block, or a wave where that is all of
+// it. Bound by HBM: 8192 x 32,000 bf16 takes 214 us, 4.9 TB/s; 100,000 rows of 100 a
+// wave each 40.
 template <class T, bool kEntropy, int kTeam>
 __global__ __launch_bounds__(kChunkThreads) void k_logp_grad(GradArgs a) {
   constexpr int V = 16 / sizeof(T);

@@ -6,12 +6,15 @@
 // registers. Rows of up to 1024 elements have a group within a wave, several
 // groups a block; longer ones have a block of waves each that exchange their
 // sums through LDS. Both kernels are bound by HBM: 8 and 16 operations an
-// element against 4 to 12 bytes.
+// element against 4 to 12 bytes. 16,384 x 4096 bf16 takes 52 us (5.2 TB/s) and
+// its gradient 100 (4.0), a million fp32 rows of 128 the gradient 290 (5.3); of
+// 10, 30. Rows of few bytes in all are bound by the launches.
 //
 // A row's loads are whole vectors in every lane, so that the next row's are in
 // flight while a row is worked on: the vector that would reach past the row's
 // end is moved back to end there and takes part with its last elements only,
-// and a lane without any reads that vector too.
+// and a lane without any reads that vector too. (Element by element behind
+// branches, the gradient of 16,384 x 4096 bf16 took 212 us.)
 #include "mlkv_ops.h"
 
 #include <algorithm>
@@ -221,7 +224,8 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(Nor
 // of its own columns in registers, in fp64 where a row is shorter than a vector
 // (of a handful of sums one can come out near zero; at any width: 200,000 x 500
 // fp16 156 us, 127 in fp32); a block joins them at its end, also in fp64.
-// (whole 16-bit rows a block: four waves a SIMD, 128 registers)
+// (whole 16-bit rows a block: four waves a SIMD, 128 registers; forced also
+// where that spills, 60,000 x 1021 fp16 took 245 us against 84)
 template <class T, int I, int kMost, bool kFull, bool kShort>
 __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMost && kFull ? 4 : 1) void k_layer_norm_grad(NormArgs a) {
   __shared__ float lds1[kNormMaxThreads / 64];
@@ -356,7 +360,8 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
 }
 
 // The blocks' sums to weight_grad and bias_grad, fp64 from here on: 16 columns
-// (of both arrays) a block, a column's sums taken by 64 threads in turn.
+// (of both arrays) a block, a column's sums taken by 64 threads in turn: bound by
+// the latency of their loads, 4 us for 625 blocks' sums of 1021 columns.
 constexpr int kJoinCols = 16, kJoinSlices = 64;
 template <class T>
 __global__ __launch_bounds__(kJoinCols * kJoinSlices) void k_norm_join(const float* sums, int blocks, int dim, void* dw,
@@ -384,7 +389,8 @@ __global__ __launch_bounds__(kJoinCols * kJoinSlices) void k_norm_join(const flo
 }
 
 // How a row lies on lanes: one vector a lane where that leaves the row within
-// a wave, else 16 elements.
+// a wave, else 16 elements (one vector also for blocks of up to 512: the gradient
+// of 16,384 x 4096 bf16 104 us against 99, rows of 8192 slower still).
 struct NormPlan {
   int I, G;
   bool block;  // a block a row
@@ -406,7 +412,8 @@ int blocks_max(const NormPlan& p, bool grad) {
 // The rows in equal shares: the blocks of as many rounds as the most blocks
 // need. A gradient's blocks take at least kGradRows rows where that leaves a
 // block for each unit: a block's sums are written and read, 16 bytes a column
-// against 6 or 12 a row and column.
+// against 6 or 12 a row and column (2000 x 5120 bf16 34 us with 8, 45 with 2, 39
+// with 4, 34 with 16).
 constexpr int kGradRows = 8;
 int norm_blocks(const NormPlan& p, int64_t n, bool grad) {
   const int64_t per = p.block ? 1 : kNormThreads / p.G, groups = (n + per - 1) / per;
