@@ -385,8 +385,8 @@ int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_t
  * and B are held as pairs of fp16 numbers (22 bits of an element, but none
  * below 2^-40, so that an update whose norm is far below eps loses digits) and
  * their products are summed in fp32; for bf16 updates of more than 128 rows and
- * columns A, B and the products' operands are single fp16 numbers, 11 bits, which
- * leaves an error below bf16's own rounding. G and out are of type dtype, row-major
+ * columns A, B (but for its diagonal, which is fp32) and the products' operands are
+ * single fp16 numbers, 11 bits, which leaves an error below bf16's own rounding. G and out are of type dtype, row-major
  * with rows (out_)row_stride and matrices (out_)batch_stride elements apart; out may be
  * G itself (same strides).
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.

@@ -18,10 +18,12 @@
 // For an update in bf16, 8 bits, the products take hi alone and A and B have no
 // lo: 11 bits of each operand, while X is carried on as a pair (with X in 11
 // bits a step's rounding would grow in the directions of small singular
-// values). The result is then off by 0.5 to 1.3e-3 of its norm, under bf16's
-// own 1.7e-3, at a third of the products (4096 x 4096 1.75 ms). Matrices of at
-// most kSmall rows, where it is up to 1.8e-3 and products cost little, take the
-// pairs.
+// values), and B's diagonal, most of it once X is near orthogonal, is kept apart
+// in fp32: a X + B X = (a + d) X + (B - d) X, the first with X's pair. The result is
+// then off by 0.3 to 1.2e-3 of its norm, under bf16's own 1.7e-3 (with the diagonal
+// in 11 bits up to 2.2e-3, the more the longer the rows), at a third of the
+// products (4096 x 4096 1.75 ms). Matrices of at most kSmall rows, where products
+// cost little, take the pairs.
 //
 // Products of a few hundred to 1024 rows have fewer tiles than the device has
 // units; they are bound by what one unit loads, 60 to 80 KB a us, and by launches,
@@ -197,6 +199,7 @@ struct ProdArgs {
   Planes add;    // what the epilogue adds a multiple of, read as [j][i]: A (symmetric) or X^T
   Planes out;    // written as [j][i] (A, B: symmetric; X^T)
   Planes out2;   // kApplyB: X, written as [i][j]
+  float* diag;   // single halves: B's diagonal, [batch][mp]
   User u;        // kApplyLast
   Shape s;
   int k;         // padded length of the sum
@@ -426,6 +429,7 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
   // bytes in 16-byte pieces: written straight from these registers a row is
   // four pieces of 16 bytes, or its other side 2 bytes a lane (1024 x 4096 B X in
   // single halves 23.8 us, 28.0 straight; 4096 x 4096 in pairs 384 and 411).
+  constexpr bool kSingleB = kPlanes == 1 && kStep == kSquareA;
   constexpr bool kPairIn = kPlanes == 2 || !kSym, kPairOut = kPlanes == 2 || kStep == kApplyB;
   constexpr int kRow = 40;  // halves of a row there: 16 bytes more than it holds, against bank conflicts
   __syncthreads();
@@ -457,6 +461,12 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
       const int i0 = bi * kTile + oi + x * 32, j0 = bj * kTile + oj + y * 32;
       if (i0 >= rows_i || j0 >= rows_j) continue;  // (sides are padded to whole blocks)
       const int il = (lane >> 5) * 4, jl = lane & 31;
+      float4 d[4] = {};  // B's diagonal at the rows
+      if constexpr (kPlanes == 1 && !kSym) {
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+          d[f] = *reinterpret_cast<const float4*>(a.diag + (int64_t)blockIdx.z * a.s.mp + i0 + f * 8 + il);
+      }
       if constexpr (kStep != kSquareX) {
         const _Float16* add = a.add.p + blockIdx.z * a.add.batch + (int64_t)j0 * a.add.ld + i0;
         load_block(add, a.add.ld, mine);
@@ -474,11 +484,22 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
           const half4 h = *reinterpret_cast<const half4*>(mine + jl * kRow + f * 8 + il);
           half4 l = {};
           if constexpr (kPairIn) l = *reinterpret_cast<const half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il);
+          const float by[4] = {kA + d[f].x, kA + d[f].y, kA + d[f].z, kA + d[f].w};  // rows' multiples of X
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float old = (float)h[e] + (float)l[e];
             v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, sum[x][y][f * 4 + e], kB * 0.5f * old)
-                                     : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], kA * old);
+                                     : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], by[e] * old);
+          }
+        }
+        if constexpr (kSingleB) {
+          if (bi == bj) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (i0 + f * 8 + il + e == j0 + jl) {
+                a.diag[(int64_t)blockIdx.z * a.s.mp + j0 + jl] = v[e] * 0x1p-14f;
+                v[e] = 0.0f;
+              }
           }
         }
         if constexpr (kStep == kApplyLast) {
@@ -796,7 +817,7 @@ __global__ __launch_bounds__(kPanelThreads) void k_orth_panel(User u, PanelWork 
 struct Layout {
   Shape s;
   int64_t xs, as;  // elements of a plane of X and of A
-  int64_t sums, bytes;  // offset of the sums of squares; all
+  int64_t sums, diag, bytes;  // offsets of the sums of squares and of B's diagonals; all
   int nsums;            // of a matrix
   int panels;           // of a matrix of few rows, or 0
 };
@@ -822,7 +843,8 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   l.as = (int64_t)l.s.mp * l.s.mp;
   // X, two of X^T, A and B, two planes each
   l.sums = up(batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16), 256);
-  l.bytes = l.sums + sums;
+  l.diag = up(l.sums + sums, 16);
+  l.bytes = l.diag + batch * l.s.mp * (int64_t)sizeof(float);
   return l;
 }
 
@@ -894,13 +916,14 @@ hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
 
 template <class T, int kPlanes>
 hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, hipStream_t st, Planes X, Planes XT0,
-                   Planes XT1, Planes A, Planes B) {
+                   Planes XT1, Planes A, Planes B, float* diag) {
   Planes now = XT0, next = XT1;
   for (int k = 0; k < steps; ++k) {
     const bool last = k + 1 == steps;
     ProdArgs a{};
     a.s = l.s;
     a.u = u;
+    a.diag = diag;
     a.P = a.Q = X;
     a.out = A;
     a.k = l.s.np;
@@ -966,6 +989,7 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   const Planes X = planes(l.xs, l.s.np), XT0 = planes(l.xs, l.s.mp), XT1 = planes(l.xs, l.s.mp),
                A = planes(l.as, l.s.mp), B = planes(l.as, l.s.mp);
   double* sums = reinterpret_cast<double*>(work + l.sums);
+  float* diag = reinterpret_cast<float*>(work + l.diag);
   hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -977,8 +1001,8 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
                      (int)rows, (int)cols);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if constexpr (std::is_same<T, bf16>::value)
-    if (single) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B);
-  return iterate<T, 2>(l, u, batch, steps, st, X, XT0, XT1, A, B);
+    if (single) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B, diag);
+  return iterate<T, 2>(l, u, batch, steps, st, X, XT0, XT1, A, B, diag);
 }
 
 int check_sizes(int64_t batch, int64_t rows, int64_t cols) {

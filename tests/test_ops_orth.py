@@ -101,6 +101,25 @@ def test_large(gen, rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(1620, 142), (130, 3900), (512, 8192), (300, 300), (700, 5000)])
+@pytest.mark.parametrize("noise", [False, True])
+def test_bf16_is_off_by_less_than_its_rounding(gen, rows, cols, noise):
+    """Two errors that have nothing to do with each other add by their squares: with one below the rounding to bf16,
+    both are below its sqrt(2)."""
+    from paper_2504_01506_amd import ops
+    m = min(rows, cols)
+    g = torch.randn(rows, cols, generator=gen, device="cuda")
+    if not noise:
+        k = m // 8
+        left = torch.randn(rows, k, generator=gen, device="cuda") * torch.logspace(0, -2, k, device="cuda")
+        g += left @ torch.randn(k, cols, generator=gen, device="cuda")
+    g = (0.01 * g).bfloat16()
+    want = reference(g, 5, 1e-7)[0]
+    off = (ops.orthogonalize(g).double() - want).norm().item()
+    assert off <= math.sqrt(2) * (want.bfloat16().double() - want).norm().item()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
 def test_steps_and_scales(gen, steps):
     for scale in (1e-6, 1.0, 1e4):
