@@ -27,7 +27,7 @@
 //
 // Products of a few hundred to 1024 rows have fewer tiles than the device has
 // units; they are bound by what one unit loads, 60 to 80 KB a us, and by launches,
-// three a step: 1024 x 4096 bf16 235 us (X X^T 15 a step on 136 tiles, A A 7.5, B X
+// three a step: 1024 x 4096 bf16 241 us (X X^T 15 a step on 136 tiles, A A 7.5, B X
 // 23, 8 of it the traffic of X), 512 x 512 fp32 136.
 #include "mlkv_ops.h"
 
@@ -858,10 +858,13 @@ using Tile256 = Tile<256, 2, 4, 1, 32, 131072>;
 // kernels measured, us a tile on a unit of its own, for 32 of k (pairs and
 // single halves) and beside that (symmetric results, and X with X^T).
 //
-// Large tiles read less for a product, 4096 x 4096 B X in pairs 411 us with 256,
-// 442 with 128, 650 with 64; but tiles come in rounds of one a unit: the 253 tiles
-// of 192 of a symmetric result of 4096 take 226 us, its 136 of 256 266, its 528
-// of 128 295. At most one round of 64 and sums of kLongSum or more: four waves by
+// Large tiles read less for a product, 4096 x 4096 B X in pairs 370 us with 256,
+// 430 with 128, 630 with 64; but tiles come in rounds of one a unit: the 253 tiles
+// of 192 of a symmetric result of 4096 take 220 us, its 136 of 256 264, its 528
+// of 128 287. Two of 128 or 64 fit a unit, so that a last round that is not full
+// takes less, beside the one before: 276 of 128 take 1.6 times what 256 do (2944 x
+// 3968, X X^T and A A 348 us, with 136 of 192 394).
+// At most one round of 64 and sums of kLongSum or more: four waves by
 // pieces of k (1024 x 4096 X X^T in single halves 16 us, 26 in quarters; in
 // pairs 36 and 41; sums of 300 8.1 and 6.5).
 constexpr int kLongSum = 1024;
@@ -880,7 +883,10 @@ int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, int planes, bool
   for (const TileTime& t : kTimes) {
     const int64_t ti = (a.s.mp + t.side - 1) / t.side, tj = (a.s.np + t.side - 1) / t.side;
     const int64_t tiles = batch * (symmetric ? ti * (ti + 1) / 2 : ti * tj), rounds = (tiles + kUnits - 1) / kUnits;
-    const float time = (float)rounds * (t.depth[2 - planes] * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
+    const float part = (float)(tiles % kUnits) / kUnits;
+    const bool beside = rounds > 1 && part > 0.0f && t.side <= 128;
+    const float taken = beside ? (float)(rounds - 1) + 0.6f + 0.4f * part : (float)rounds;
+    const float time = taken * (t.depth[2 - planes] * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
     if (best == 0 || time < least) {
       best = t.side;
       least = time;
