@@ -384,10 +384,10 @@ int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_t
  * with (a, b, c) = (3.4445, -4.7750, 2.0315). The norm is summed in fp64. X, A
  * and B are held as pairs of fp16 numbers (22 bits of an element, but none
  * below 2^-40, so that an update whose norm is far below eps loses digits) and
- * their products are summed in fp32; for bf16 updates of more than 128 rows and
- * columns A, B (but for its diagonal, which is fp32) and the products' operands are
- * single fp16 numbers, 11 bits, which leaves an error below bf16's own rounding. G and out are of type dtype, row-major
- * with rows (out_)row_stride and matrices (out_)batch_stride elements apart; out may be
+ * their products are summed in fp32, whatever dtype is: errors of the size of
+ * those of the steps in fp32, which each step stretches, in directions of small
+ * singular values up to 3.4445 times. G and out are of type dtype, row-major with
+ * rows (out_)row_stride and matrices (out_)batch_stride elements apart; out may be
  * G itself (same strides).
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.
  * 0 <= batch <= 65535, 1 <= rows, cols <= MLKV_ORTH_MAX_DIM, 1 <= steps <= 64,

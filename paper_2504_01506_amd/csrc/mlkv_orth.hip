@@ -15,20 +15,15 @@
 // steps of 4096 x 4096 take 4.1 ms, 1.0 PFLOP/s of fp16 products, of which a large
 // library product reaches 1.08.
 //
-// For an update in bf16, 8 bits, the products take hi alone and A and B have no
-// lo: 11 bits of each operand, while X is carried on as a pair (with X in 11
-// bits a step's rounding would grow in the directions of small singular
-// values), and B's diagonal, most of it once X is near orthogonal, is kept apart
-// in fp32: a X + B X = (a + d) X + (B - d) X, the first with X's pair. The result is
-// then off by 0.3 to 1.2e-3 of its norm, under bf16's own 1.7e-3 (with the diagonal
-// in 11 bits up to 2.2e-3, the more the longer the rows), at a third of the
-// products (4096 x 4096 1.75 ms). Matrices of at most kSmall rows, where products
-// cost little, take the pairs.
+// Updates in bf16 and fp16 take the same pairs: what a step rounds off lies in
+// the directions of small singular values too, and each later step stretches it
+// there by up to 3.4445. With operands of 11 bits a result is off by 0.7e-3 of its norm
+// (noise, 5 steps) to 2.4e-2 (low rank, 8 steps), bf16's own rounding being
+// 1.7e-3; with pairs by about as much as the steps in fp32.
 //
 // Products of a few hundred to 1024 rows have fewer tiles than the device has
 // units; they are bound by what one unit loads, 60 to 80 KB a us, and by launches,
-// three a step: 1024 x 4096 bf16 241 us (X X^T 15 a step on 136 tiles, A A 7.5, B X
-// 23, 8 of it the traffic of X), 512 x 512 fp32 136.
+// three a step: 1024 x 4096 425 us, 1024 x 1024 192, 512 x 512 136.
 #include "mlkv_ops.h"
 
 #include <algorithm>
@@ -42,7 +37,7 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kThreads = 256;
 constexpr int kPad = 64;         // sides of X and A are padded to multiples of it, with zeros
 constexpr int kNormBlocks = 512; // sums of squares a matrix, at most
-constexpr int kSmall = 128;
+constexpr int kPlanes = 2;       // hi and lo
 
 using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
@@ -113,7 +108,7 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
   lo = (_Float16)(v - (float)hi);
 }
 
-// Planes of one matrix: hi at p, lo `plane` elements behind it (to k_orth_begin 0: no lo).
+// Planes of one matrix: hi at p, lo `plane` elements behind it.
 struct Planes {
   _Float16* p;
   int64_t plane, batch;
@@ -121,9 +116,8 @@ struct Planes {
 };
 
 // X and X^T from G, 64 x 64 elements a block, 8 a thread at a time, the
-// transposed ones through LDS. Bound by memory: 2 or 4 bytes read and 6 or 8
-// written an element (1024 x 4096 bf16 8 to 10 us, an element at a time 15; 4096 x
-// 4096 fp32 31, 6.5 TB/s).
+// transposed ones through LDS. Bound by memory: 2 or 4 bytes read and 8 written
+// an element (4096 x 4096 fp32 31 us, 6.5 TB/s).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, const double* sums, int nsums, float eps, Planes straight,
                                                          Planes turned, int rows, int cols) {
@@ -162,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_begin(User u, const double* s
       lo[e] = l;
     }
     *reinterpret_cast<half8*>(at) = hi;
-    if (to.plane != 0) *reinterpret_cast<half8*>(at + to.plane) = lo;
+    *reinterpret_cast<half8*>(at + to.plane) = lo;
   };
   // (sides are padded to whole tiles, with zeros)
   _Float16* a = straight.p + blockIdx.z * straight.batch + (int64_t)r0 * straight.ld + c0;
@@ -199,7 +193,6 @@ struct ProdArgs {
   Planes add;    // what the epilogue adds a multiple of, read as [j][i]: A (symmetric) or X^T
   Planes out;    // written as [j][i] (A, B: symmetric; X^T)
   Planes out2;   // kApplyB: X, written as [i][j]
-  float* diag;   // single halves: B's diagonal, [batch][mp]
   User u;        // kApplyLast
   Shape s;
   int k;         // padded length of the sum
@@ -243,7 +236,7 @@ struct Tile {
 
 // kStages stages in LDS: while one is multiplied, the others are on their way
 // from memory.
-template <class T, class Tile_, int kPlanes, int kStep>
+template <class T, class Tile_, int kStep>
 __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) {
   constexpr int kTile = Tile_::side, kDepth = Tile_::depth, kWaves = Tile_::waves;
   constexpr int kBi = Tile_::blocks_i, kBj = Tile_::blocks_j, kOi = Tile_::out_i, kOj = Tile_::out_j;
@@ -339,18 +332,16 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
 #pragma unroll
       for (int y = 0; y < kBj; ++y)
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][0], s.q[y][0], acc[x][y], 0, 0, 0);
-    if constexpr (kPlanes == 2) {
 #pragma unroll
-      for (int x = 0; x < kBi; ++x)
+    for (int x = 0; x < kBi; ++x)
 #pragma unroll
-        for (int y = 0; y < kBj; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][0], s.q[y][1], acc[x][y], 0, 0, 0);
+      for (int y = 0; y < kBj; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][0], s.q[y][1], acc[x][y], 0, 0, 0);
 #pragma unroll
-      for (int x = 0; x < kBi; ++x)
+    for (int x = 0; x < kBi; ++x)
 #pragma unroll
-        for (int y = 0; y < kBj; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][1], s.q[y][0], acc[x][y], 0, 0, 0);
-    }
+      for (int y = 0; y < kBj; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s.p[x][1], s.q[y][0], acc[x][y], 0, 0, 0);
   };
   if constexpr (Tile_::waves_k > 1) {
     // a wave has one piece of a stage: it reads the next while it multiplies this one
@@ -427,10 +418,8 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
   // Epilogue. A lane holds column j = lane % 32 of each block, rows i in fours.
   // Blocks go to and from memory through LDS, a wave's own 5 KB, as rows of 64
   // bytes in 16-byte pieces: written straight from these registers a row is
-  // four pieces of 16 bytes, or its other side 2 bytes a lane (1024 x 4096 B X in
-  // single halves 23.8 us, 28.0 straight; 4096 x 4096 in pairs 384 and 411).
-  constexpr bool kSingleB = kPlanes == 1 && kStep == kSquareA;
-  constexpr bool kPairIn = kPlanes == 2 || !kSym, kPairOut = kPlanes == 2 || kStep == kApplyB;
+  // four pieces of 16 bytes, or its other side 2 bytes a lane (4096 x 4096 B X 384
+  // us, 411 straight).
   constexpr int kRow = 40;  // halves of a row there: 16 bytes more than it holds, against bank conflicts
   __syncthreads();
   _Float16* mine = lds + wave * (2 * 32 * kRow);
@@ -461,16 +450,10 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
       const int i0 = bi * kTile + oi + x * 32, j0 = bj * kTile + oj + y * 32;
       if (i0 >= rows_i || j0 >= rows_j) continue;  // (sides are padded to whole blocks)
       const int il = (lane >> 5) * 4, jl = lane & 31;
-      float4 d[4] = {};  // B's diagonal at the rows
-      if constexpr (kPlanes == 1 && !kSym) {
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-          d[f] = *reinterpret_cast<const float4*>(a.diag + (int64_t)blockIdx.z * a.s.mp + i0 + f * 8 + il);
-      }
       if constexpr (kStep != kSquareX) {
         const _Float16* add = a.add.p + blockIdx.z * a.add.batch + (int64_t)j0 * a.add.ld + i0;
         load_block(add, a.add.ld, mine);
-        if constexpr (kPairIn) load_block(add + a.add.plane, a.add.ld, mine + 32 * kRow);
+        load_block(add + a.add.plane, a.add.ld, mine + 32 * kRow);
         wave_sync();
       }
       half4 hi[4], lo[4];
@@ -482,24 +465,12 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
           for (int e = 0; e < 4; ++e) v[e] = sum[x][y][f * 4 + e] * 0x1p-15f;
         } else {
           const half4 h = *reinterpret_cast<const half4*>(mine + jl * kRow + f * 8 + il);
-          half4 l = {};
-          if constexpr (kPairIn) l = *reinterpret_cast<const half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il);
-          const float by[4] = {kA + d[f].x, kA + d[f].y, kA + d[f].z, kA + d[f].w};  // rows' multiples of X
+          const half4 l = *reinterpret_cast<const half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float old = (float)h[e] + (float)l[e];
             v[e] = kStep == kSquareA ? __builtin_fmaf(kC * 0x1p-16f, sum[x][y][f * 4 + e], kB * 0.5f * old)
-                                     : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], by[e] * old);
-          }
-        }
-        if constexpr (kSingleB) {
-          if (bi == bj) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (i0 + f * 8 + il + e == j0 + jl) {
-                a.diag[(int64_t)blockIdx.z * a.s.mp + j0 + jl] = v[e] * 0x1p-14f;
-                v[e] = 0.0f;
-              }
+                                     : __builtin_fmaf(0x1p-14f, sum[x][y][f * 4 + e], kA * old);
           }
         }
         if constexpr (kStep == kApplyLast) {
@@ -526,12 +497,12 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
           *reinterpret_cast<half4*>(mine + jl * kRow + f * 8 + il) = hi[f];
-          if constexpr (kPairOut) *reinterpret_cast<half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il) = lo[f];
+          *reinterpret_cast<half4*>(mine + 32 * kRow + jl * kRow + f * 8 + il) = lo[f];
         }
         wave_sync();
         _Float16* out = a.out.p + blockIdx.z * a.out.batch + (int64_t)j0 * a.out.ld + i0;
         store_block(mine, out, a.out.ld);
-        if constexpr (kPairOut) store_block(mine + 32 * kRow, out + a.out.plane, a.out.ld);
+        store_block(mine + 32 * kRow, out + a.out.plane, a.out.ld);
         wave_sync();
         if (kStep == kApplyB || (kSym && bi != bj)) {
           const Planes& o = kSym ? a.out : a.out2;
@@ -540,13 +511,12 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               mine[(f * 8 + il + e) * kRow + jl] = hi[f][e];
-              // (X's lo is not read by products of single halves)
-              if constexpr (kPlanes == 2) mine[(32 + f * 8 + il + e) * kRow + jl] = lo[f][e];
+              mine[(32 + f * 8 + il + e) * kRow + jl] = lo[f][e];
             }
           wave_sync();
           _Float16* to = o.p + blockIdx.z * o.batch + (int64_t)i0 * o.ld + j0;
           store_block(mine, to, o.ld);
-          if constexpr (kPlanes == 2) store_block(mine + 32 * kRow, to + o.plane, o.ld);
+          store_block(mine + 32 * kRow, to + o.plane, o.ld);
           wave_sync();
         }
       }
@@ -817,7 +787,7 @@ __global__ __launch_bounds__(kPanelThreads) void k_orth_panel(User u, PanelWork 
 struct Layout {
   Shape s;
   int64_t xs, as;  // elements of a plane of X and of A
-  int64_t sums, diag, bytes;  // offsets of the sums of squares and of B's diagonals; all
+  int64_t sums, bytes;  // offset of the sums of squares; all
   int nsums;            // of a matrix
   int panels;           // of a matrix of few rows, or 0
 };
@@ -843,8 +813,7 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
   l.as = (int64_t)l.s.mp * l.s.mp;
   // X, two of X^T, A and B, two planes each
   l.sums = up(batch * (l.xs * 6 + l.as * 4) * (int64_t)sizeof(_Float16), 256);
-  l.diag = up(l.sums + sums, 16);
-  l.bytes = l.diag + batch * l.s.mp * (int64_t)sizeof(float);
+  l.bytes = l.sums + sums;
   return l;
 }
 
@@ -855,29 +824,28 @@ using Tile192 = Tile<192, 2, 2, 1, 32, 98304>;
 using Tile256 = Tile<256, 2, 4, 1, 32, 131072>;
 
 // Which tile a product takes: that of the least time by a fit to what the
-// kernels measured, us a tile on a unit of its own, for 32 of k (pairs and
-// single halves) and beside that (symmetric results, and X with X^T).
+// kernels measured, us a tile on a unit of its own, for 32 of k and beside that
+// (symmetric results, and X with X^T).
 //
-// Large tiles read less for a product, 4096 x 4096 B X in pairs 370 us with 256,
+// Large tiles read less for a product, 4096 x 4096 B X 370 us with 256,
 // 430 with 128, 630 with 64; but tiles come in rounds of one a unit: the 253 tiles
 // of 192 of a symmetric result of 4096 take 220 us, its 136 of 256 264, its 528
 // of 128 287. Two of 128 or 64 fit a unit, so that a last round that is not full
 // takes less, beside the one before: 276 of 128 take 1.6 times what 256 do (2944 x
 // 3968, X X^T and A A 348 us, with 136 of 192 394).
 // At most one round of 64 and sums of kLongSum or more: four waves by
-// pieces of k (1024 x 4096 X X^T in single halves 16 us, 26 in quarters; in
-// pairs 36 and 41; sums of 300 8.1 and 6.5).
+// pieces of k (1024 x 4096 X X^T 36 us, 41 in quarters; sums of 300 8.1 and 6.5).
 constexpr int kLongSum = 1024;
 struct TileTime {
   int side;
-  float depth[2], rest[2];
+  float depth, rest[2];
 };
-constexpr TileTime kTimes[] = {{64, {0.34f, 0.15f}, {2.5f, 2.7f}},
-                               {128, {0.9f, 0.4f}, {5.0f, 11.0f}},
-                               {192, {1.75f, 0.75f}, {8.0f, 20.0f}},
-                               {256, {3.2f, 1.5f}, {10.0f, 16.0f}}};
+constexpr TileTime kTimes[] = {{64, 0.34f, {2.5f, 2.7f}},
+                               {128, 0.9f, {5.0f, 11.0f}},
+                               {192, 1.75f, {8.0f, 20.0f}},
+                               {256, 3.2f, {10.0f, 16.0f}}};
 constexpr int kUnits = 256;
-int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, int planes, bool* one_round) {
+int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, bool* one_round) {
   int best = 0;
   float least = 0.0f;
   for (const TileTime& t : kTimes) {
@@ -886,7 +854,7 @@ int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, int planes, bool
     const float part = (float)(tiles % kUnits) / kUnits;
     const bool beside = rounds > 1 && part > 0.0f && t.side <= 128;
     const float taken = beside ? (float)(rounds - 1) + 0.6f + 0.4f * part : (float)rounds;
-    const float time = taken * (t.depth[2 - planes] * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
+    const float time = taken * (t.depth * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
     if (best == 0 || time < least) {
       best = t.side;
       least = time;
@@ -896,54 +864,53 @@ int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, int planes, bool
   return best;
 }
 
-template <class T, class Tile_, int kPlanes, int kStep>
+template <class T, class Tile_, int kStep>
 hipError_t product_of(ProdArgs a, int64_t batch, hipStream_t st) {
   constexpr bool kSym = kStep == kSquareX || kStep == kSquareA;
   a.ti = (a.s.mp + Tile_::side - 1) / Tile_::side;
   a.tj = kSym ? a.ti : (a.s.np + Tile_::side - 1) / Tile_::side;
   const unsigned tiles = kSym ? (unsigned)(a.ti * (a.ti + 1) / 2) : (unsigned)(a.ti * a.tj);
-  const hipError_t e = allow_lds<k_orth_product<T, Tile_, kPlanes, kStep>>(Tile_::lds);
+  const hipError_t e = allow_lds<k_orth_product<T, Tile_, kStep>>(Tile_::lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_orth_product<T, Tile_, kPlanes, kStep>), dim3(tiles, 1, (unsigned)batch),
+  hipLaunchKernelGGL((k_orth_product<T, Tile_, kStep>), dim3(tiles, 1, (unsigned)batch),
                      dim3(64 * Tile_::waves), Tile_::lds, st, a);
   return hipGetLastError();
 }
 
-template <class T, int kPlanes, int kStep>
+template <class T, int kStep>
 hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
   bool one_round = false;
-  const int side = tile_side(a, batch, kStep == kSquareX || kStep == kSquareA, kPlanes, &one_round);
-  if (side == 64 && one_round && a.k >= kLongSum) return product_of<T, Tile64K, kPlanes, kStep>(a, batch, st);
-  if (side == 64) return product_of<T, Tile64, kPlanes, kStep>(a, batch, st);
-  if (side == 128) return product_of<T, Tile128, kPlanes, kStep>(a, batch, st);
-  if (side == 192) return product_of<T, Tile192, kPlanes, kStep>(a, batch, st);
-  return product_of<T, Tile256, kPlanes, kStep>(a, batch, st);
+  const int side = tile_side(a, batch, kStep == kSquareX || kStep == kSquareA, &one_round);
+  if (side == 64 && one_round && a.k >= kLongSum) return product_of<T, Tile64K, kStep>(a, batch, st);
+  if (side == 64) return product_of<T, Tile64, kStep>(a, batch, st);
+  if (side == 128) return product_of<T, Tile128, kStep>(a, batch, st);
+  if (side == 192) return product_of<T, Tile192, kStep>(a, batch, st);
+  return product_of<T, Tile256, kStep>(a, batch, st);
 }
 
-template <class T, int kPlanes>
+template <class T>
 hipError_t iterate(const Layout& l, const User& u, int64_t batch, int steps, hipStream_t st, Planes X, Planes XT0,
-                   Planes XT1, Planes A, Planes B, float* diag) {
+                   Planes XT1, Planes A, Planes B) {
   Planes now = XT0, next = XT1;
   for (int k = 0; k < steps; ++k) {
     const bool last = k + 1 == steps;
     ProdArgs a{};
     a.s = l.s;
     a.u = u;
-    a.diag = diag;
     a.P = a.Q = X;
     a.out = A;
     a.k = l.s.np;
-    hipError_t e = product<float, kPlanes, kSquareX>(a, batch, st);
+    hipError_t e = product<float, kSquareX>(a, batch, st);
     if (e != hipSuccess) return e;
     a.P = a.Q = a.add = A;
     a.out = B;
     a.k = l.s.mp;
-    if ((e = product<float, kPlanes, kSquareA>(a, batch, st)) != hipSuccess) return e;
+    if ((e = product<float, kSquareA>(a, batch, st)) != hipSuccess) return e;
     a.P = B;
     a.Q = a.add = now;
     a.out = next;
     a.out2 = X;
-    e = last ? product<T, kPlanes, kApplyLast>(a, batch, st) : product<float, kPlanes, kApplyB>(a, batch, st);
+    e = last ? product<T, kApplyLast>(a, batch, st) : product<float, kApplyB>(a, batch, st);
     if (e != hipSuccess) return e;
     std::swap(now, next);
   }
@@ -995,20 +962,14 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   const Planes X = planes(l.xs, l.s.np), XT0 = planes(l.xs, l.s.mp), XT1 = planes(l.xs, l.s.mp),
                A = planes(l.as, l.s.mp), B = planes(l.as, l.s.mp);
   double* sums = reinterpret_cast<double*>(work + l.sums);
-  float* diag = reinterpret_cast<float*>(work + l.diag);
   hipLaunchKernelGGL((k_orth_norm<T>), dim3(l.nsums, (unsigned)batch), dim3(kThreads), 0, st, u, rows, cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const bool single = std::is_same<T, bf16>::value && l.s.m > kSmall;
-  Planes first = X;
-  if (single) first.plane = 0;
   hipLaunchKernelGGL((k_orth_begin<T>), dim3((unsigned)(cols + 63) / 64, (unsigned)(rows + 63) / 64, (unsigned)batch),
-                     dim3(kThreads), 0, st, u, sums, l.nsums, eps, l.s.turned ? XT0 : first, l.s.turned ? first : XT0,
+                     dim3(kThreads), 0, st, u, sums, l.nsums, eps, l.s.turned ? XT0 : X, l.s.turned ? X : XT0,
                      (int)rows, (int)cols);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if constexpr (std::is_same<T, bf16>::value)
-    if (single) return iterate<T, 1>(l, u, batch, steps, st, X, XT0, XT1, A, B, diag);
-  return iterate<T, 2>(l, u, batch, steps, st, X, XT0, XT1, A, B, diag);
+  return iterate<T>(l, u, batch, steps, st, X, XT0, XT1, A, B);
 }
 
 int check_sizes(int64_t batch, int64_t rows, int64_t cols) {
