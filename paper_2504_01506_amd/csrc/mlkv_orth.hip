@@ -421,8 +421,14 @@ __global__ __launch_bounds__(64 * Tile_::waves) void k_orth_product(ProdArgs a) 
   // four pieces of 16 bytes, or its other side 2 bytes a lane (4096 x 4096 B X 384
   // us, 411 straight).
   constexpr int kRow = 40;  // halves of a row there: 16 bytes more than it holds, against bank conflicts
-  __syncthreads();
-  _Float16* mine = lds + wave * (2 * 32 * kRow);
+  // These 5 KB lie behind the parts of the sum, where there are such: in the
+  // parts' place a wave would write them before another has read its own. (A
+  // barrier between did not hold that: the compiler takes reads of LDS whose values
+  // only one branch needs into that branch, also past a barrier before it.)
+  constexpr int kParts = Tile_::waves_k > 1 ? kWaves * 4 * 4 * 64 * (int)(sizeof(float4) / sizeof(_Float16)) : 0;
+  static_assert((kParts + kWaves * 2 * 32 * kRow) * (int)sizeof(_Float16) <= Tile_::lds, "LDS of the epilogue");
+  if constexpr (Tile_::waves_k == 1) __syncthreads();
+  _Float16* mine = lds + kParts + wave * (2 * 32 * kRow);
   // the block's rows of a plane from LDS, or to it; `from` and `to` point at the block's corner
   const auto store_block = [&](const _Float16* from, _Float16* to, int ld) {
 #pragma unroll
