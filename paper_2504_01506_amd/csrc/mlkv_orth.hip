@@ -25,6 +25,7 @@
 // units; they are bound by what one unit loads, 60 to 80 KB a us, and by launches,
 // three a step: 1024 x 4096 425 us, 1024 x 1024 192, 512 x 512 136.
 #include "mlkv_ops.h"
+#include "mlkv_tiles.h"
 
 #include <algorithm>
 #include <atomic>
@@ -35,7 +36,6 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kThreads = 256;
-constexpr int kPad = 64;         // sides of X and A are padded to multiples of it, with zeros
 constexpr int kNormBlocks = 512; // sums of squares a matrix, at most
 constexpr int kPlanes = 2;       // hi and lo
 
@@ -813,8 +813,8 @@ Layout layout(int64_t batch, int64_t rows, int64_t cols) {
     l.bytes = l.panels == 1 ? 0 : l.sums + sums;
     return l;
   }
-  l.s.mp = (int)up(l.s.m, kPad);
-  l.s.np = (int)up(l.s.n, kPad);
+  l.s.mp = (int)up(l.s.m, kOrthPad);
+  l.s.np = (int)up(l.s.n, kOrthPad);
   l.xs = (int64_t)l.s.mp * l.s.np;
   l.as = (int64_t)l.s.mp * l.s.mp;
   // X, two of X^T, A and B, two planes each
@@ -828,47 +828,6 @@ using Tile64 = Tile<64, 2, 2, 1, 32, 65536>;
 using Tile128 = Tile<128, 2, 2, 1, 32, 65536>;
 using Tile192 = Tile<192, 2, 2, 1, 32, 98304>;
 using Tile256 = Tile<256, 2, 4, 1, 32, 131072>;
-
-// Which tile a product takes: that of the least time by a fit to what the
-// kernels measured, us a tile on a unit of its own, for 32 of k and beside that
-// (symmetric results, and X with X^T).
-//
-// Large tiles read less for a product, 4096 x 4096 B X 370 us with 256,
-// 430 with 128, 630 with 64; but tiles come in rounds of one a unit: the 253 tiles
-// of 192 of a symmetric result of 4096 take 220 us, its 136 of 256 264, its 528
-// of 128 287. Two of 128 or 64 fit a unit, so that a last round that is not full
-// takes less, beside the one before: 276 of 128 take 1.6 times what 256 do (2944 x
-// 3968, X X^T and A A 348 us, with 136 of 192 394).
-// At most one round of 64 and sums of kLongSum or more: four waves by
-// pieces of k (1024 x 4096 X X^T 36 us, 41 in quarters; sums of 300 8.1 and 6.5).
-constexpr int kLongSum = 1024;
-struct TileTime {
-  int side;
-  float depth, rest[2];
-};
-constexpr TileTime kTimes[] = {{64, 0.34f, {2.5f, 2.7f}},
-                               {128, 0.9f, {5.0f, 11.0f}},
-                               {192, 1.75f, {8.0f, 20.0f}},
-                               {256, 3.2f, {10.0f, 16.0f}}};
-constexpr int kUnits = 256;
-int tile_side(const ProdArgs& a, int64_t batch, bool symmetric, bool* one_round) {
-  int best = 0;
-  float least = 0.0f;
-  for (const TileTime& t : kTimes) {
-    const int64_t ti = (a.s.mp + t.side - 1) / t.side, tj = (a.s.np + t.side - 1) / t.side;
-    const int64_t tiles = batch * (symmetric ? ti * (ti + 1) / 2 : ti * tj), rounds = (tiles + kUnits - 1) / kUnits;
-    const float part = (float)(tiles % kUnits) / kUnits;
-    const bool beside = rounds > 1 && part > 0.0f && t.side <= 128;
-    const float taken = beside ? (float)(rounds - 1) + 0.6f + 0.4f * part : (float)rounds;
-    const float time = taken * (t.depth * (float)(a.k / 32) + t.rest[symmetric ? 0 : 1]);
-    if (best == 0 || time < least) {
-      best = t.side;
-      least = time;
-      *one_round = rounds == 1;
-    }
-  }
-  return best;
-}
 
 template <class T, class Tile_, int kStep>
 hipError_t product_of(ProdArgs a, int64_t batch, hipStream_t st) {
@@ -885,12 +844,13 @@ hipError_t product_of(ProdArgs a, int64_t batch, hipStream_t st) {
 
 template <class T, int kStep>
 hipError_t product(const ProdArgs& a, int64_t batch, hipStream_t st) {
-  bool one_round = false;
-  const int side = tile_side(a, batch, kStep == kSquareX || kStep == kSquareA, &one_round);
-  if (side == 64 && one_round && a.k >= kLongSum) return product_of<T, Tile64K, kStep>(a, batch, st);
-  if (side == 64) return product_of<T, Tile64, kStep>(a, batch, st);
-  if (side == 128) return product_of<T, Tile128, kStep>(a, batch, st);
-  if (side == 192) return product_of<T, Tile192, kStep>(a, batch, st);
+  switch (orth_tile(a.s.mp, a.s.np, batch, kStep == kSquareX || kStep == kSquareA, a.k)) {
+    case OrthTile::k64K: return product_of<T, Tile64K, kStep>(a, batch, st);
+    case OrthTile::k64: return product_of<T, Tile64, kStep>(a, batch, st);
+    case OrthTile::k128: return product_of<T, Tile128, kStep>(a, batch, st);
+    case OrthTile::k192: return product_of<T, Tile192, kStep>(a, batch, st);
+    case OrthTile::k256: break;
+  }
   return product_of<T, Tile256, kStep>(a, batch, st);
 }
 
