@@ -387,8 +387,9 @@ int mlkv_log_probs_grad(const void *d_logits, int64_t stride, const int64_t *d_t
  * their products are summed in fp32, whatever dtype is: errors of the size of
  * those of the steps in fp32, which each step stretches, in directions of small
  * singular values up to 3.4445 times. G and out are of type dtype, row-major with
- * rows (out_)row_stride and matrices (out_)batch_stride elements apart; out may be
- * G itself (same strides).
+ * rows (out_)row_stride and matrices (out_)batch_stride elements apart (matrices
+ * one behind another, or their rows in turn: heads side by side in a weight's
+ * rows); out may be G itself (same strides).
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN.
  * 0 <= batch <= 65535, 1 <= rows, cols <= MLKV_ORTH_MAX_DIM, 1 <= steps <= 64,
  * eps > 0 and finite.

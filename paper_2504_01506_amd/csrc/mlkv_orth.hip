@@ -972,8 +972,12 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (!stride_ok(row_stride, rows, cols, true) || !stride_ok(out_row_stride, rows, cols, false))
     return op_error(MLKV_EINVAL, "row strides must be >= cols (or 0 in g)");
+  // out's matrices one behind another, or their rows in turn (a matrix a head, heads side by side in a row)
   const int64_t span = (rows - 1) * (rows > 1 ? out_row_stride : 0) + cols;
-  if (batch > 1 && (batch_stride < 0 || batch_stride > (int64_t(1) << 44) || !stride_ok(out_batch_stride, batch, span, false)))
+  if (batch > 1 && (batch_stride < 0 || batch_stride > (int64_t(1) << 44) ||
+                    !(stride_ok(out_batch_stride, batch, span, false) ||
+                      (stride_ok(out_batch_stride, batch, cols, false) &&
+                       out_row_stride >= (batch - 1) * out_batch_stride + cols))))
     return op_error(MLKV_EINVAL, "batch strides must not make matrices overlap");
   if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))
     return op_error(MLKV_EINVAL, "out may be g only with the same strides");
