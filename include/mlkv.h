@@ -299,7 +299,10 @@ int mlkv_read_staleness(mlkv_table *t, const int64_t *d_rows, int64_t n, uint32_
  * disturb each other as long as their buffers differ (workspaces included).
  * Rows lie `*_stride` ELEMENTS apart (>= the row's length, or 0 in an input
  * whose rows are all the same; any alignment of the element type), the elements of a
- * row next to each other. Arguments are checked before anything is launched:
+ * row next to each other. A call writes where it says and reads nothing that it
+ * writes: outputs overlap no other buffer of the call but where an output may be
+ * an input; rows of output that overlap rows of input otherwise are refused.
+ * Arguments are checked before anything is launched:
  * MLKV_EINVAL leaves every buffer as it was. Equal calls on equal data, at
  * addresses that are equal modulo 16 bytes, give equal bits. */
 

@@ -497,6 +497,10 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (d_out == d_x && n > 1 && x_stride != out_stride)
     return op_error(MLKV_EINVAL, "out may be x only with the same stride");
+  const RowSpan x{d_x, x_stride * size, n, (int64_t)dim * size}, out{d_out, out_stride * size, n, (int64_t)dim * size};
+  const int64_t params = (int64_t)dim * wsize;
+  if (!out_ok(x, out) || rows_meet({d_weight, 0, 1, params}, out) || rows_meet({d_bias, 0, 1, params}, out))
+    return op_error(MLKV_EINVAL, "out overlaps x, weight or bias");
   const NormPlan p = norm_plan(dim, size);
   NormArgs a{};
   a.x = d_x;
@@ -545,6 +549,11 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   if (n > 1 && d_x_grad != nullptr &&
       ((d_x_grad == d_x && x_grad_stride != x_stride) || (d_x_grad == d_grad && x_grad_stride != grad_stride)))
     return op_error(MLKV_EINVAL, "x_grad may be x or grad only with the same stride");
+  const int64_t width = (int64_t)dim * size;
+  const RowSpan x{d_x, x_stride * size, n, width}, grad{d_grad, grad_stride * size, n, width},
+      x_grad{d_x_grad, x_grad_stride * size, n, width};
+  if (!out_ok(x, x_grad) || !out_ok(grad, x_grad) || rows_meet({d_weight, 0, 1, (int64_t)dim * wsize}, x_grad))
+    return op_error(MLKV_EINVAL, "x_grad overlaps x, grad or weight");
   if (sums && n > 0) {
     if (d_work == nullptr || work_bytes < mlkv_layer_norm_grad_workspace(n, dim))
       return op_error(MLKV_EINVAL, "work is smaller than mlkv_layer_norm_grad_workspace");

@@ -5,7 +5,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <initializer_list>
+#include <numeric>
 #include <type_traits>
 
 #include "mlkv.h"
@@ -47,6 +49,62 @@ inline bool stride_ok(int64_t stride, int64_t rows, int64_t width, bool same) {
   if (rows <= 1) return true;
   if (same && stride == 0) return true;
   return stride >= width && stride <= (int64_t(1) << 60) / rows;
+}
+
+// `rows` rows of `width` bytes, `stride` bytes apart, as stride_ok has passed them.
+struct RowSpan {
+  const void* p;
+  int64_t stride, rows, width;
+};
+
+// Whether a byte of a's rows is one of b's; b's rows do not overlap each other.
+// Exact, so that rows side by side in one buffer are told apart: at once where
+// the strides are equal or leave the rows apart in every common period, else
+// row by row of a (up to the first that meets b's).
+inline bool rows_meet(RowSpan a, RowSpan b) {
+  using Wide = __int128;  // (addresses and their differences)
+  if (a.p == nullptr || b.p == nullptr || a.rows <= 0 || b.rows <= 0) return false;
+  if (a.stride == 0 || a.rows == 1) a.rows = 1, a.stride = 0;
+  if (b.rows == 1) b.stride = 0;
+  const Wide at = (Wide)reinterpret_cast<uintptr_t>(b.p) - (Wide)reinterpret_cast<uintptr_t>(a.p);  // b from a
+  if (at >= (Wide)(a.rows - 1) * a.stride + a.width || -at >= (Wide)(b.rows - 1) * b.stride + b.width) return false;
+  const auto floor_div = [](Wide x, Wide y) { return x / y - (x % y < 0); };
+  if (a.stride != 0 && b.stride != 0) {
+    const int64_t period = std::gcd(a.stride, b.stride);
+    const Wide in = at - floor_div(at, period) * period;
+    if (in >= a.width && in + b.width <= period) return false;
+    if (a.stride == b.stride && a.width <= a.stride) {
+      // row i of a and row i - m of b: at - m stride apart
+      for (Wide m = floor_div(at, a.stride); m <= floor_div(at, a.stride) + 1; ++m) {
+        const Wide apart = at - m * a.stride;
+        if (m < a.rows && -m < b.rows && apart < a.width && -apart < b.width) return true;
+      }
+      return false;
+    }
+  }
+  // (the rows of a from the first that reaches b's on, to the last)
+  const Wide reach = (Wide)(b.rows - 1) * b.stride + b.width;
+  int64_t i = 0, end = a.rows;
+  if (a.stride != 0) {
+    i = (int64_t)std::max<Wide>(floor_div(at - a.width, a.stride) + 1, 0);
+    end = (int64_t)std::min<Wide>(floor_div(at + reach - 1, a.stride) + 1, a.rows);
+  }
+  for (; i < end; ++i) {
+    const Wide from = (Wide)i * a.stride - at;  // row i of a from b's first
+    if (b.stride == 0) {
+      if (from < b.width && -from < a.width) return true;
+      continue;
+    }
+    const Wide first = std::max<Wide>(floor_div(from - b.width, b.stride) + 1, 0);
+    const Wide last = std::min<Wide>(floor_div(from + a.width - 1, b.stride), b.rows - 1);
+    if (first <= last) return true;
+  }
+  return false;
+}
+
+// Whether output rows may lie there: they are the input's own, in place, or share no byte with them.
+inline bool out_ok(const RowSpan& in, const RowSpan& out) {
+  return (in.p == out.p && (in.rows <= 1 || in.stride == out.stride)) || !rows_meet(in, out);
 }
 
 // V elements of T as one load or store at any address that T may have: 16

@@ -938,6 +938,42 @@ hipError_t orthogonalize(const Layout& l, const User& u, int64_t batch, int64_t 
   return iterate<T>(l, u, batch, steps, st, X, XT0, XT1, A, B);
 }
 
+// A stack of matrices: `n` things `step` bytes apart, each `rows` rows of
+// `width` bytes, `stride` apart; the longer way is the outer one.
+struct Stack {
+  int64_t step, n;
+  RowSpan one;
+  int64_t span() const { return (one.rows - 1) * one.stride + one.width; }
+};
+Stack stack_of(const void* p, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows, int64_t width) {
+  if (batch <= 1 || batch_stride == 0) batch = 1, batch_stride = 0;
+  if (rows <= 1 || row_stride == 0) rows = 1, row_stride = 0;
+  if (batch > 1 && (rows == 1 || row_stride <= batch_stride))
+    return {batch_stride, batch, {p, row_stride, rows, width}};
+  return {row_stride, rows, {p, batch_stride, batch, width}};
+}
+
+// Whether a byte of G's is one of out's, whose rows do not overlap: at once
+// where both lie apart as a whole or each thing of the outer way does, else
+// thing by thing.
+bool stacks_meet(const Stack& g, const Stack& out) {
+  if (!rows_meet({g.one.p, g.step, g.n, g.span()}, {out.one.p, out.step, out.n, out.span()})) return false;
+  for (int64_t i = 0; i < g.n; ++i) {
+    RowSpan a = g.one;
+    a.p = static_cast<const char*>(a.p) + i * g.step;
+    const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(a.p) - reinterpret_cast<uintptr_t>(out.one.p));
+    const int64_t step = std::max<int64_t>(out.step, 1);
+    const int64_t first = std::max<int64_t>((from - out.span()) / step, 0);
+    const int64_t last = std::min((from + g.span()) / step, out.n - 1);
+    for (int64_t j = first; j <= last; ++j) {
+      RowSpan b = out.one;
+      b.p = static_cast<const char*>(b.p) + j * out.step;
+      if (rows_meet(a, b)) return true;
+    }
+  }
+  return false;
+}
+
 int check_sizes(int64_t batch, int64_t rows, int64_t cols) {
   if (batch < 0 || batch > 65535) return op_error(MLKV_EINVAL, "batch must be in [0, 65535]");
   if (rows < 1 || rows > MLKV_ORTH_MAX_DIM || cols < 1 || cols > MLKV_ORTH_MAX_DIM)
@@ -981,6 +1017,9 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
     return op_error(MLKV_EINVAL, "batch strides must not make matrices overlap");
   if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))
     return op_error(MLKV_EINVAL, "out may be g only with the same strides");
+  if (d_out != d_g && stacks_meet(stack_of(d_g, batch_stride * size, row_stride * size, batch, rows, cols * size),
+                                  stack_of(d_out, out_batch_stride * size, out_row_stride * size, batch, rows, cols * size)))
+    return op_error(MLKV_EINVAL, "out overlaps g");
   const Layout l = layout(batch, rows, cols);
   if (l.bytes > 0 && (d_work == nullptr || work_bytes < l.bytes))
     return op_error(MLKV_EINVAL, "work is smaller than mlkv_orthogonalize_workspace");
