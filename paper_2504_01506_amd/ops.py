@@ -8,7 +8,10 @@ computes): tensors are checked here and passed as device pointers, outputs and
 workspaces that are not given are allocated by torch, and the work is queued on
 `stream` (the current stream of the tensors' device unless given) without
 waiting for it. They stand outside torch's autograd: gradients are calls of
-their own. There is no fallback: without the built library, or on tensors
+their own, and while autograd records, a tensor that requires a gradient is
+refused (call under torch.no_grad(), on tensor.detach(), or from the forward and
+backward of a torch.autograd.Function). What is written to a given `out` counts
+as a change of it in place. There is no fallback: without the built library, or on tensors
 that are not on a GPU, a call raises.
 
 As with any torch call on a side stream, a tensor that is given and was made on
@@ -59,6 +62,21 @@ def _on_gpu(t: torch.Tensor, what: str):
         raise ValueError(f"{what} must be a tensor on a GPU")
     if t.is_conj() or t.is_neg():
         raise ValueError(f"{what} must be resolved first")
+
+
+def _no_graph(*tensors):
+    """Refuses tensors that autograd would expect a gradient for: the result has no history."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if getattr(t, "requires_grad", False):
+                raise ValueError("the dense operators are not recorded by autograd: call them under torch.no_grad(), "
+                                 "on tensor.detach(), or from a torch.autograd.Function")
+
+
+def _changed(out: Optional[torch.Tensor]):
+    """Tells autograd that a given output has been written."""
+    if out is not None:
+        torch.autograd.graph.increment_version(out)
 
 
 def _rows(t: torch.Tensor, what: str) -> tuple[int, int, int]:
@@ -143,6 +161,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                eps: float = 1e-5, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Layer norm over the last dimension of x ([..., dim], fp32, bf16 or fp16);
     weight and bias ([dim], fp32 or of x's type) may be None. `out` may be x."""
+    _no_graph(x, weight, bias, out)
     _on_gpu(x, "x")
     kind = _dtype(x, "x")
     n, dim, step = _rows(x, "x")
@@ -153,10 +172,11 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     p = weight if weight is not None else bias
     wkind = kind if p is None else _TYPES[p.dtype]
     with _Queue(x, stream) as st:
-        out, ostep = _out_rows(out, x, dim)
+        y, ystep = _out_rows(out, x, dim)
         mlkv._check(mlkv.load().mlkv_layer_norm(x.data_ptr(), step, _ptr(weight), _ptr(bias), n, dim, eps, kind, wkind,
-                                                out.data_ptr(), ostep, st))
-    return out
+                                                y.data_ptr(), ystep, st))
+    _changed(out)
+    return y
 
 
 def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch.Tensor, eps: float = 1e-5,
@@ -165,6 +185,7 @@ def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch
     the gradient `grad` of its output. x_grad is of x's type (rows for a
     table's put_grad where that is fp32) and goes to `out` if given (which may
     be grad or x); the other two are of weight's type, or x's without a weight."""
+    _no_graph(x, weight, grad, out)
     _on_gpu(x, "x")
     kind = _dtype(x, "x")
     n, dim, step = _rows(x, "x")
@@ -173,16 +194,17 @@ def layer_norm_grad(x: torch.Tensor, weight: Optional[torch.Tensor], grad: torch
     _check(grad, "grad", x, x.dtype, x.shape)
     gstep = _rows(grad, "grad")[2]
     with _Queue(x, stream) as st:
-        out, ostep = _out_rows(out, x, dim)
+        dx, dstep = _out_rows(out, x, dim)
         dw = x.new_empty(dim) if weight is None else torch.empty_like(weight)
         db = torch.empty_like(dw)
         lib = mlkv.load()
         nbytes = _bytes(lib.mlkv_layer_norm_grad_workspace(n, dim))
         work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
         mlkv._check(lib.mlkv_layer_norm_grad(x.data_ptr(), step, _ptr(weight), grad.data_ptr(), gstep, n, dim, eps, kind,
-                                             wkind, out.data_ptr(), ostep, dw.data_ptr(), db.data_ptr(),
+                                             wkind, dx.data_ptr(), dstep, dw.data_ptr(), db.data_ptr(),
                                              work.data_ptr(), nbytes, st))
-    return out, dw, db
+    _changed(out)
+    return dx, dw, db
 
 
 class LogProbs(NamedTuple):
@@ -197,6 +219,7 @@ def log_probs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, stream=N
     """Log probability of tokens[...] (int64; < 0: none, gives 0) under
     logits[..., vocab], the distribution's entropy, and the `top` (<= 64) most
     likely alternatives. `stats` and `entropy` are what log_probs_grad takes."""
+    _no_graph(logits)
     _on_gpu(logits, "logits")
     kind = _dtype(logits, "logits")
     n, vocab, step = _rows(logits, "logits")
@@ -223,6 +246,7 @@ def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: 
                    stream=None) -> torch.Tensor:
     """Gradient in the logits, for the gradients logp_grad and entropy_grad
     (fp32, either may be None) of log_probs' first two outputs; `out` may be logits."""
+    _no_graph(logits, stats, entropy, logp_grad, entropy_grad, out)
     _on_gpu(logits, "logits")
     kind = _dtype(logits, "logits")
     n, vocab, step = _rows(logits, "logits")
@@ -241,11 +265,12 @@ def log_probs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: 
     if entropy is not None:
         _check(entropy, "entropy", logits, torch.float32, lead, dense=True)
     with _Queue(logits, stream) as st:
-        out, ostep = _out_rows(out, logits, vocab)
+        grad, gstep = _out_rows(out, logits, vocab)
         mlkv._check(mlkv.load().mlkv_log_probs_grad(logits.data_ptr(), step, _ptr(tokens), stats.data_ptr(),
                                                     _ptr(entropy), _ptr(logp_grad), _ptr(entropy_grad), n, vocab, kind,
-                                                    out.data_ptr(), ostep, st))
-    return out
+                                                    grad.data_ptr(), gstep, st))
+    _changed(out)
+    return grad
 
 
 def _matrices(t: torch.Tensor, what: str) -> tuple[int, int]:
@@ -264,6 +289,7 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
     fp32, bf16 or fp16) made nearly orthogonal by `steps` Newton-Schulz steps:
     the same singular vectors, singular values near 1. `out` may be g. A
     transposed view is taken as it lies: its transpose is worked on."""
+    _no_graph(g, out)
     _on_gpu(g, "g")
     kind = _dtype(g, "g")
     if g.dim() not in (2, 3):
@@ -277,13 +303,15 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
     gb, gr = _matrices(g, "g")
     with _Queue(g, stream) as st:
         if out is None:
-            out = torch.empty_like(g, memory_format=torch.contiguous_format)
+            x = torch.empty_like(g, memory_format=torch.contiguous_format)
         else:
+            x = out
             _check(out, "out", g, g.dtype, g.shape)
-        ob, orow = _matrices(out, "out")
+        xb, xr = _matrices(x, "out")
         lib = mlkv.load()
         nbytes = _bytes(lib.mlkv_orthogonalize_workspace(batch, rows, cols))
         work = torch.empty(nbytes, dtype=torch.uint8, device=g.device) if nbytes else None
         mlkv._check(lib.mlkv_orthogonalize(g.data_ptr(), gb, gr, batch, rows, cols, int(steps), eps, kind,
-                                           out.data_ptr(), ob, orow, _ptr(work), nbytes, st))
-    return out
+                                           x.data_ptr(), xb, xr, _ptr(work), nbytes, st))
+    _changed(out)
+    return x
