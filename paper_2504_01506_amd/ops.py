@@ -283,12 +283,18 @@ def _matrices(t: torch.Tensor, what: str) -> tuple[int, int]:
     return t.stride(0), row
 
 
+def _standing(t: torch.Tensor) -> bool:
+    """Whether t's matrices are transposed views: columns' elements next to each other."""
+    return t.stride(-1) != 1 and t.stride(-2) == 1 and t.shape[-1] > 1
+
+
 def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
     """The update g ([rows, cols], or [batch, rows, cols] for a stack of them;
     fp32, bf16 or fp16) made nearly orthogonal by `steps` Newton-Schulz steps:
     the same singular vectors, singular values near 1. `out` may be g. A
-    transposed view is taken as it lies: its transpose is worked on."""
+    transposed view is taken as it lies: its transpose is worked on (one of g and
+    `out` alone: the result is copied from a buffer of its own)."""
     _no_graph(g, out)
     _on_gpu(g, "g")
     kind = _dtype(g, "g")
@@ -296,17 +302,20 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, eps: float = 1e-7, out: Optio
         raise ValueError("g must have 2 or 3 dimensions")
     if g.shape[-1] == 0 or g.shape[-2] == 0:
         raise ValueError("g has matrices of no elements")
-    if g.stride(-1) != 1 and g.stride(-2) == 1 and g.shape[-1] > 1:
-        return orthogonalize(g.mT, steps, eps, None if out is None else out.mT, stream).mT
+    if out is not None:
+        _check(out, "out", g, g.dtype, g.shape)
+        if _standing(g) != _standing(out):
+            _matrices(out.mT if _standing(out) else out, "out")
+            with _Queue(g, stream):
+                return out.copy_(orthogonalize(g, steps, eps))
+    if _standing(g):
+        x = orthogonalize(g.mT, steps, eps, None if out is None else out.mT, stream).mT
+        return x if out is None else out
     batch = g.shape[0] if g.dim() == 3 else 1
     rows, cols = g.shape[-2:]
     gb, gr = _matrices(g, "g")
     with _Queue(g, stream) as st:
-        if out is None:
-            x = torch.empty_like(g, memory_format=torch.contiguous_format)
-        else:
-            x = out
-            _check(out, "out", g, g.dtype, g.shape)
+        x = torch.empty_like(g, memory_format=torch.contiguous_format) if out is None else out
         xb, xr = _matrices(x, "out")
         lib = mlkv.load()
         nbytes = _bytes(lib.mlkv_orthogonalize_workspace(batch, rows, cols))

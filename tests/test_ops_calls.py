@@ -156,3 +156,44 @@ def test_rows_side_by_side_in_one_buffer(gen):
                 lambda: ops.orthogonalize(stack[:4], out=stack[2:])):
         with pytest.raises(mlkv.MlkvError, match="overlaps"):
             bad()
+
+
+# ---- transposed views ----
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(70, 200), (200, 70), (3, 40, 90), (50, 50), (1, 9), (9, 1), (2, 1, 30)])
+def test_transposed_views_on_either_side(gen, shape):
+    from paper_2504_01506_amd import ops
+    lying = torch.randn(shape, generator=gen, device="cuda")
+    standing = lying.mT.contiguous().mT
+    side = torch.cuda.Stream()
+    for g in (lying, standing):
+        want = ops.orthogonalize(g)     # (a square's transpose takes other sums)
+        for like in (lying, standing):
+            for stream in (None, side):
+                out = torch.empty_like(like)     # (keeps the strides)
+                torch.cuda.synchronize()
+                assert ops.orthogonalize(g, out=out, stream=stream) is out
+                torch.cuda.synchronize()
+                assert torch.equal(out, want)
+    assert torch.equal(ops.orthogonalize(standing, out=standing), want)
+
+
+@pytest.mark.gpu
+def test_a_square_into_its_transpose(gen):
+    from paper_2504_01506_amd import ops
+    w = torch.randn((90, 90), generator=gen, device="cuda")
+    want = ops.orthogonalize(w.t())
+    assert torch.equal(ops.orthogonalize(w.t(), out=w), want) and torch.equal(w, want)
+
+
+@pytest.mark.gpu
+def test_outputs_that_lie_neither_way_are_refused(gen):
+    from paper_2504_01506_amd import ops
+    g = torch.randn((40, 60), generator=gen, device="cuda")
+    hold = torch.zeros((40, 120), device="cuda")
+    for bad in (g, g.t().contiguous().t()):
+        with pytest.raises((ValueError, RuntimeError)):
+            ops.orthogonalize(bad, out=hold[:, ::2])
+        with pytest.raises((ValueError, RuntimeError)):
+            ops.orthogonalize(bad, out=hold[:1, :60].expand(40, 60))
+    assert (hold == 0).all()
