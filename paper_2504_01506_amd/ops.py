@@ -55,6 +55,8 @@ def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=Non
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
+    if t.is_neg():
+        raise ValueError(f"{what} must be resolved first")
 
 
 def _on_gpu(t: torch.Tensor, what: str):

@@ -197,3 +197,34 @@ def test_outputs_that_lie_neither_way_are_refused(gen):
         with pytest.raises((ValueError, RuntimeError)):
             ops.orthogonalize(bad, out=hold[:1, :60].expand(40, 60))
     assert (hold == 0).all()
+
+
+# ---- views whose memory holds their negative ----
+@pytest.mark.gpu
+def test_views_that_stand_for_their_negative_are_refused(gen):
+    from paper_2504_01506_amd import ops
+    x, w = torch.randn((6, 8), generator=gen, device="cuda"), torch.randn(8, generator=gen, device="cuda")
+    t = torch.zeros(6, dtype=torch.int64, device="cuda")
+    r = ops.log_probs(x, t)
+    neg = torch._neg_view
+    for bad in (lambda: ops.layer_norm(neg(x)), lambda: ops.layer_norm(x, neg(w)), lambda: ops.layer_norm(x, w, neg(w)),
+                lambda: ops.layer_norm(x, out=neg(x)), lambda: ops.layer_norm_grad(x, None, neg(x)),
+                lambda: ops.layer_norm_grad(x, None, x, out=neg(x)), lambda: ops.log_probs(neg(x), t),
+                lambda: ops.log_probs_grad(x, t, neg(r.stats), None, r.logp),
+                lambda: ops.log_probs_grad(x, t, r.stats, None, neg(r.logp)),
+                lambda: ops.log_probs_grad(x, t, r.stats, neg(r.entropy), r.logp, r.logp),
+                lambda: ops.log_probs_grad(x, t, r.stats, None, r.logp, out=neg(x)),
+                lambda: ops.orthogonalize(neg(x)), lambda: ops.orthogonalize(x, out=neg(x))):
+        with pytest.raises(ValueError, match="resolved"):
+            bad()
+    # (rows of one element from the imaginary part of a conjugate)
+    grad = torch.complex(x[:, :1], x[:, 1:2]).conj().imag
+    with pytest.raises(ValueError, match="resolved"):
+        ops.layer_norm_grad(x[:, :1], None, grad)
+
+
+def test_a_view_that_stands_for_its_negative_is_no_argument():
+    from paper_2504_01506_amd import ops
+    x = torch.ones(4)
+    with pytest.raises(ValueError, match="resolved"):
+        ops._check(torch._neg_view(x), "weight", x)
