@@ -223,14 +223,15 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(Nor
 // needs: of d = x - mean, d^2, g and g d. Each thread keeps the sums over rows
 // of its own columns in registers, in fp64 where a row is shorter than a vector
 // (of a handful of sums one can come out near zero; at any width: 200,000 x 500
-// fp16 156 us, 127 in fp32); a block joins them at its end, also in fp64.
+// fp16 156 us, 127 in fp32); a block joins them at its end, in fp64, and leaves
+// its sums in fp32 (rounded once) for k_norm_join.
 // (whole 16-bit rows a block: four waves a SIMD, 128 registers; forced also
 // where that spills, 60,000 x 1021 fp16 took 245 us against 84)
 template <class T, int I, int kMost, bool kFull, bool kShort>
 __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMost && kFull ? 4 : 1) void k_layer_norm_grad(NormArgs a) {
   __shared__ float lds1[kNormMaxThreads / 64];
   __shared__ __align__(16) float lds2[4 * kNormMaxThreads / 64];
-  extern __shared__ __align__(16) float join[];  // [groups of the block, or its waves][G * I * V] (not kBlock)
+  extern __shared__ __align__(16) float join[];  // of Sum: [groups of the block, or its waves][G * I * V] (not kBlock)
   constexpr int V = 16 / sizeof(T);
   constexpr bool kBlock = kMost != 0, kAhead = kMost != kNormMaxThreads;
   const int G = a.G, l = kBlock ? threadIdx.x : threadIdx.x & (G - 1), dim = a.dim;
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
         for (int e = 0; e < V; ++e) {
           double t = which ? db[e] : dw[e];
           for (int o = 1; o < 64; o *= 2) t += __shfl_xor(t, o);
-          if ((threadIdx.x & 63) == 0) join[threadIdx.x / 64 * V + e] = (float)t;
+          if ((threadIdx.x & 63) == 0) reinterpret_cast<double*>(join)[threadIdx.x / 64 * V + e] = t;
         }
       } else {
 #pragma unroll
@@ -349,11 +350,12 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
       for (int c = threadIdx.x; c < dim; c += kNormThreads) {
         // column c's place: in the last vector of the row the elements are at its end
         const int first = c / V * V, at = kFull || kShort || first + V <= dim ? c : c + V - (dim - first);
-        double t = 0.0;
+        const auto* sums = reinterpret_cast<const Sum*>(join);
+        double t[4] = {};
         for (int k = 0; k < parts; k += 4)  // (a power of two from 4 on)
-          t += (double)((join[k * width + at] + join[(k + 1) * width + at]) +
-                        (join[(k + 2) * width + at] + join[(k + 3) * width + at]));
-        mine[which * dim + c] = (float)t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] += (double)sums[(k + e) * width + at];
+        mine[which * dim + c] = (float)((t[0] + t[1]) + (t[2] + t[3]));
       }
     }
   }
