@@ -26,9 +26,12 @@ import torch
 
 from . import mlkv
 
-# a stream's handle without the Stream object around it (a microsecond and a half a call), where torch has that
+# a stream's handle without the Stream object around it (a microsecond and a half a call), and the current device
+# without a look at whether torch has started the GPU (a tensor is there), where torch has those
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_recording = torch.is_grad_enabled
 
 _TYPES = {torch.float32: mlkv.MLKV_F32, torch.bfloat16: mlkv.MLKV_BF16, torch.float16: mlkv.MLKV_F16}
 
@@ -47,7 +50,7 @@ def _dtype(t: torch.Tensor, what: str) -> int:
 def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=None, dense=False):
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{what} must be a tensor")
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{what} is on {t.device}, not on {like.device}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
@@ -60,17 +63,17 @@ def _check(t: torch.Tensor, what: str, like: torch.Tensor, dtype=None, shape=Non
 
 
 def _on_gpu(t: torch.Tensor, what: str):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a tensor on a GPU")
-    if t.is_conj() or t.is_neg():
+    if t.is_neg():
         raise ValueError(f"{what} must be resolved first")
 
 
 def _no_graph(*tensors):
     """Refuses tensors that autograd would expect a gradient for: the result has no history."""
-    if torch.is_grad_enabled():
+    if _recording():
         for t in tensors:
-            if getattr(t, "requires_grad", False):
+            if t is not None and getattr(t, "requires_grad", False):
                 raise ValueError("the dense operators are not recorded by autograd: call them under torch.no_grad(), "
                                  "on tensor.detach(), or from a torch.autograd.Function")
 
@@ -126,7 +129,7 @@ class _Queue:
         self.device, self.stream, self.held = t.device, stream, None
 
     def __enter__(self) -> int:
-        if self.stream is None and self.device.index == torch.cuda.current_device():
+        if self.stream is None and self.device.index == _current_device():
             return _raw_stream(self.device.index)
         s = self.stream
         if s is None:
