@@ -834,7 +834,7 @@ int check_logits(const void* logits, int64_t stride, int64_t n, int64_t vocab, i
   if (size == 0) return op_error(MLKV_EINVAL, "unknown dtype");
   if (n > 0 && logits == nullptr) return op_error(MLKV_EINVAL, "logits is NULL");
   if (!stride_ok(stride, n, vocab, true)) return op_error(MLKV_EINVAL, "stride must be 0 or >= vocab");
-  if (!all_aligned(size, size, {logits}, {}))
+  if (!all_aligned(size, {logits}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   return MLKV_OK;
 }
@@ -867,13 +867,13 @@ int mlkv_log_probs(const void* d_logits, int64_t stride, const int64_t* d_tokens
   if (d_logp != nullptr && d_tokens == nullptr && n > 0) return op_error(MLKV_EINVAL, "tokens is NULL");
   if (top == 0 && (d_top_ids != nullptr || d_top_logp != nullptr))
     return op_error(MLKV_EINVAL, "top_ids and top_logp must be NULL with top = 0");
-  if (!all_aligned(8, 1, {d_tokens, d_top_ids}, {}) ||
-      !all_aligned(4, 1, {d_logp, d_entropy, d_stats, d_top_logp}, {}))
+  if (!all_aligned(8, {d_tokens, d_top_ids}) ||
+      !all_aligned(4, {d_logp, d_entropy, d_stats, d_top_logp}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (bytes > 0) {
     if (d_work == nullptr || work_bytes < bytes)
       return op_error(MLKV_EINVAL, "work is smaller than mlkv_log_probs_workspace");
-    if (!all_aligned(16, 1, {d_work}, {})) return op_error(MLKV_EINVAL, "work must be at a multiple of 16 bytes");
+    if (!all_aligned(16, {d_work})) return op_error(MLKV_EINVAL, "work must be at a multiple of 16 bytes");
   }
   if (n == 0) return MLKV_OK;
   const ChunkPlan c = chunk_plan(n, vocab, dtype_size(dtype));
@@ -914,8 +914,8 @@ int mlkv_log_probs_grad(const void* d_logits, int64_t stride, const int64_t* d_t
     if (d_entropy_grad != nullptr && d_entropy == nullptr) return op_error(MLKV_EINVAL, "entropy is NULL");
   }
   if (!stride_ok(grad_stride, n, vocab, false)) return op_error(MLKV_EINVAL, "grad_stride must be >= vocab");
-  if (!all_aligned(size, size, {d_logits_grad}, {}) || !all_aligned(8, 1, {d_tokens}, {}) ||
-      !all_aligned(4, 1, {d_stats, d_entropy, d_logp_grad, d_entropy_grad}, {}))
+  if (!all_aligned(size, {d_logits_grad}) || !all_aligned(8, {d_tokens}) ||
+      !all_aligned(4, {d_stats, d_entropy, d_logp_grad, d_entropy_grad}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (n > 1 && d_logits_grad == d_logits && stride != grad_stride)
     return op_error(MLKV_EINVAL, "logits_grad may be logits only with the same stride");

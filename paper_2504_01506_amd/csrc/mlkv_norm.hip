@@ -495,7 +495,7 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
   if (d_out == nullptr) return op_error(MLKV_EINVAL, "out is NULL");
   if (!stride_ok(out_stride, n, dim, false)) return op_error(MLKV_EINVAL, "out_stride must be >= dim");
   const int size = dtype_size(dtype), wsize = dtype_size(weight_dtype);
-  if (!all_aligned(size, size, {d_x, d_out}, {}) || !all_aligned(wsize, wsize, {d_weight, d_bias}, {}))
+  if (!all_aligned(size, {d_x, d_out}) || !all_aligned(wsize, {d_weight, d_bias}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (d_out == d_x && n > 1 && x_stride != out_stride)
     return op_error(MLKV_EINVAL, "out may be x only with the same stride");
@@ -545,8 +545,8 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   if (!stride_ok(grad_stride, n, dim, true)) return op_error(MLKV_EINVAL, "grad_stride must be 0 or >= dim");
   if (d_x_grad != nullptr && !stride_ok(x_grad_stride, n, dim, false))
     return op_error(MLKV_EINVAL, "x_grad_stride must be >= dim");
-  if (!all_aligned(size, size, {d_x, d_grad, d_x_grad}, {}) ||
-      !all_aligned(wsize, wsize, {d_weight, d_weight_grad, d_bias_grad}, {}))
+  if (!all_aligned(size, {d_x, d_grad, d_x_grad}) ||
+      !all_aligned(wsize, {d_weight, d_weight_grad, d_bias_grad}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (n > 1 && d_x_grad != nullptr &&
       ((d_x_grad == d_x && x_grad_stride != x_stride) || (d_x_grad == d_grad && x_grad_stride != grad_stride)))
@@ -559,7 +559,7 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   if (sums && n > 0) {
     if (d_work == nullptr || work_bytes < mlkv_layer_norm_grad_workspace(n, dim))
       return op_error(MLKV_EINVAL, "work is smaller than mlkv_layer_norm_grad_workspace");
-    if (!all_aligned(16, 1, {d_work}, {})) return op_error(MLKV_EINVAL, "work must be at a multiple of 16 bytes");
+    if (!all_aligned(16, {d_work})) return op_error(MLKV_EINVAL, "work must be at a multiple of 16 bytes");
   }
   if (!sums && (n == 0 || d_x_grad == nullptr)) return MLKV_OK;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);

@@ -33,12 +33,10 @@ auto dispatch_type(int dtype, F f) {
   return f(f16{});
 }
 
-// Whether all of `ptrs`, and the strides in elements of `size` bytes, are multiples of `bytes`.
-inline bool all_aligned(size_t bytes, size_t size, std::initializer_list<const void*> ptrs,
-                        std::initializer_list<int64_t> strides) {
+// Whether all of `ptrs` are multiples of `bytes`.
+inline bool all_aligned(size_t bytes, std::initializer_list<const void*> ptrs) {
   uintptr_t x = 0;
   for (const void* p : ptrs) x |= reinterpret_cast<uintptr_t>(p);
-  for (int64_t s : strides) x |= static_cast<uintptr_t>(s) * size;
   return x % bytes == 0;
 }
 

@@ -1004,7 +1004,7 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
   if (!(eps > 0.0f) || std::isinf(eps)) return op_error(MLKV_EINVAL, "eps must be finite and > 0");
   if (batch == 0) return MLKV_OK;
   if (d_g == nullptr || d_out == nullptr) return op_error(MLKV_EINVAL, "g or out is NULL");
-  if (!all_aligned(size, size, {d_g, d_out}, {}))
+  if (!all_aligned(size, {d_g, d_out}))
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (!stride_ok(row_stride, rows, cols, true) || !stride_ok(out_row_stride, rows, cols, false))
     return op_error(MLKV_EINVAL, "row strides must be >= cols (or 0 in g)");
@@ -1023,7 +1023,7 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
   const Layout l = layout(batch, rows, cols);
   if (l.bytes > 0 && (d_work == nullptr || work_bytes < l.bytes))
     return op_error(MLKV_EINVAL, "work is smaller than mlkv_orthogonalize_workspace");
-  if (l.bytes > 0 && !all_aligned(256, 1, {d_work}, {}))
+  if (l.bytes > 0 && !all_aligned(256, {d_work}))
     return op_error(MLKV_EINVAL, "work must be at a multiple of 256 bytes");
   User u;
   u.g = d_g;
