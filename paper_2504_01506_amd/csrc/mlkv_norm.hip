@@ -211,8 +211,8 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(Nor
         LoosePack<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          o.v[j] = (T)__builtin_fmaf((x[i * V + j] - off) * rstd, w[i * V + j], b[i * V + j]);
-        // (elements that are another lane's too get the same value from both)
+          o.v[j] = rounded<T>(__builtin_fmaf((x[i * V + j] - off) * rstd, w[i * V + j], b[i * V + j]));
+        // (elements that are another lane's too get the same value from both, to the last bit)
         if (kFull || kShort || cols.skip[i] < V) store_row<T, V, kShort>(out, cols.at[i], dim, o);
       }
     }
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
           const float h = (x[i * V + j] - off) * rstd, dy = element<T>(gr[i], j);
           // (kShort: g rounded as it was for its mean, so that a row of one element gets 0)
           const float g_over = kShort ? dy * w[i * V + j] - g_mean : __builtin_fmaf(dy, w[i * V + j], -g_mean);
-          o.v[j] = (T)(rstd * (g_over - h * gh_mean));
+          o.v[j] = rounded<T>(rstd * (g_over - h * gh_mean));
           if constexpr (std::is_same<Sum, double>::value) dw[i * V + j] = __builtin_fma((double)dy, (double)h, dw[i * V + j]);
           else dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
           db[i * V + j] += dy;
@@ -351,11 +351,12 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
         // column c's place: in the last vector of the row the elements are at its end
         const int first = c / V * V, at = kFull || kShort || first + V <= dim ? c : c + V - (dim - first);
         const auto* sums = reinterpret_cast<const Sum*>(join);
-        double t[4] = {};
-        for (int k = 0; k < parts; k += 4)  // (a power of two from 4 on)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) t[e] += (double)sums[(k + e) * width + at];
-        mine[which * dim + c] = (float)((t[0] + t[1]) + (t[2] + t[3]));
+        double t = 0.0;
+        for (int k = 0; k < parts; k += 4) {  // (a power of two from 4 on)
+          const Sum* at4 = sums + k * width + at;
+          t += ((double)at4[0] + (double)at4[width]) + ((double)at4[2 * width] + (double)at4[3 * width]);
+        }
+        mine[which * dim + c] = (float)t;
       }
     }
   }

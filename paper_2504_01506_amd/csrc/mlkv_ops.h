@@ -133,6 +133,16 @@ __device__ __forceinline__ float element(const Raw& r, int j) {
   }
 }
 
+// v as a T, rounded from fp32 wherever it stands. fp16: an operation before it
+// that the compiler takes together with the rounding (v_fma_mixlo_f16 does not
+// round to fp32 between, which in 235 of 4.2 million results shows) would make
+// an element's last bit depend on its place in a vector.
+template <class T>
+__device__ __forceinline__ T rounded(float v) {
+  if constexpr (std::is_same<T, f16>::value) asm("" : "+v"(v));
+  return (T)v;
+}
+
 // The sum of v over groups of G lanes (a power of two, at most 64), in every
 // lane of the group. All lanes of the wave must be active. Within 16 lanes by
 // data-parallel moves (xor 1, xor 2, then mirrors, which meet equal values),
