@@ -329,9 +329,9 @@ int mlkv_layer_norm(const void *d_x, int64_t x_stride, const void *d_weight, con
  *     bias_grad[c]   = sum over rows of grad[c]
  * mu and v are taken from x again. x, grad and x_grad are of type dtype (fp32
  * rows of x_grad are what mlkv_put_grad takes), weight, weight_grad and
- * bias_grad of weight_dtype. The sums over rows are fp32 in a thread (fp64 where
- * a row is shorter than 16 bytes) and fp64 over a block's threads and over the
- * blocks, each of which hands on fp32, in a fixed order; with n = 0 they are 0.
+ * bias_grad of weight_dtype. The sums over rows are fp32 in a thread and fp64 over
+ * a block's threads and over the blocks, each of which hands on fp32, in a fixed
+ * order; rows shorter than 16 bytes are fp64 throughout; with n = 0 the sums are 0.
  * d_weight may be NULL (1); d_x_grad, d_weight_grad and d_bias_grad may each
  * be NULL (not wanted). d_x_grad may be d_grad or d_x (same stride). d_work:
  * mlkv_layer_norm_grad_workspace(n, dim) bytes at a multiple of 16 (may be

@@ -34,7 +34,7 @@ struct NormArgs {
   const void* weight;  // or NULL
   const void* bias;    // or NULL
   void* out;           // or NULL (gradient)
-  float* sums;         // gradient: [blocks][2][dim], or NULL
+  void* sums;          // gradient: [blocks][2][dim] floats (doubles for rows shorter than a vector), or NULL
   int64_t x_stride, grad_stride, out_stride;
   int64_t n;
   int dim;
@@ -221,10 +221,14 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads) void k_layer_norm(Nor
 
 // The gradient. After the mean one exchange gives the four sums that the rest
 // needs: of d = x - mean, d^2, g and g d. Each thread keeps the sums over rows
-// of its own columns in registers, in fp64 where a row is shorter than a vector
-// (of a handful of sums one can come out near zero; at any width: 200,000 x 500
-// fp16 156 us, 127 in fp32); a block joins them at its end, in fp64, and leaves
-// its sums in fp32 (rounded once) for k_norm_join.
+// of its own columns in registers; a block joins them at its end, in fp64, and
+// leaves its sums in fp32 (rounded once) for k_norm_join.
+// Rows shorter than a vector are worked on, summed and left in fp64 throughout:
+// of a handful of sums one can come out near zero, and the gradient of a row of
+// one element is zero, of two all but zero (9 x 2 fp32 was off by 4e-3 of it, as
+// 32 bits are). 1M x 3 fp16 23 us, 25 in fp32; 10M x 7 fp16 311 and 296, 10M x 2 fp32
+// 46 and 52.
+// (Sums in fp64 at any width: 200,000 x 500 fp16 156 us, 127 in fp32.)
 // (whole 16-bit rows a block: four waves a SIMD, 128 registers; forced also
 // where that spills, 60,000 x 1021 fp16 took 245 us against 84)
 template <class T, int I, int kMost, bool kFull, bool kShort>
@@ -238,7 +242,7 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
   const int per = kBlock ? 1 : kNormThreads / G;
   const float inv = 1.0f / (float)dim;
   const Columns<T, I, kFull> cols(l, G, dim);
-  const auto own = [&](int i, int j) { return kShort ? j < dim : cols.own(i, j); };
+  const auto own = [&](int i, int j) { return cols.own(i, j); };
   using Sum = std::conditional_t<kShort, double, float>;
   float w[I * V];
   Sum dw[I * V], db[I * V];
@@ -258,6 +262,44 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
   if constexpr (kAhead) load(r);
   for (int64_t base = (int64_t)blockIdx.x * per; base < a.n; base += step, r += step) {
     if constexpr (!kAhead) load(r);
+    if constexpr (kShort) {
+      // (places from dim on are 0 in x and grad)
+      double x[V - 1], g[V - 1], s = 0.0, q = 0.0, g_sum = 0.0, gd = 0.0;
+#pragma unroll
+      for (int j = 0; j < V - 1; ++j) {
+        x[j] = element<T>(nx[0], j);
+        g[j] = element<T>(ng[0], j);
+        s += x[j];
+      }
+      load(r + step);
+      // (s / dim to the last bit: a row of equal elements is its mean)
+      const double over = 1.0 / dim, near = s * over, mean = __builtin_fma(__builtin_fma(-near, (double)dim, s), over, near);
+#pragma unroll
+      for (int j = 0; j < V - 1; ++j) {
+        x[j] = j < dim ? x[j] - mean : 0.0;
+        q = __builtin_fma(x[j], x[j], q);
+        g_sum += g[j] * w[j];
+        gd = __builtin_fma(g[j] * w[j], x[j], gd);
+      }
+      // 1 / sqrt: the unit's estimate and two of Newton's steps (10M x 2 fp32 46 us; divided by a root 64)
+      const double v = __builtin_fma(q, over, (double)a.eps);
+      double rstd = __builtin_amdgcn_rsq(v);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) rstd = __builtin_fma(0.5 * rstd, __builtin_fma(-v * rstd, rstd, 1.0), rstd);
+      const double g_mean = g_sum * over, gh_mean = gd * over * rstd;
+      if (r < a.n) {
+        LoosePack<T, V> o;
+#pragma unroll
+        for (int j = 0; j < V - 1; ++j) {
+          const double h = x[j] * rstd;
+          o.v[j] = (T)(float)(rstd * (g[j] * w[j] - g_mean - h * gh_mean));
+          dw[j] = __builtin_fma(g[j], h, dw[j]);
+          db[j] += g[j];
+        }
+        if (a.out != nullptr) store_row<T, V, true>(static_cast<T*>(a.out) + r * a.out_stride, 0, dim, o);
+      }
+      continue;
+    }
     float x[I * V];
     Raw gr[I];
     float s[1] = {0.0f};
@@ -299,20 +341,17 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float h = (x[i * V + j] - off) * rstd, dy = element<T>(gr[i], j);
-          // (kShort: g rounded as it was for its mean, so that a row of one element gets 0)
-          const float g_over = kShort ? dy * w[i * V + j] - g_mean : __builtin_fmaf(dy, w[i * V + j], -g_mean);
-          o.v[j] = rounded<T>(rstd * (g_over - h * gh_mean));
-          if constexpr (std::is_same<Sum, double>::value) dw[i * V + j] = __builtin_fma((double)dy, (double)h, dw[i * V + j]);
-          else dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
+          o.v[j] = rounded<T>(rstd * (__builtin_fmaf(dy, w[i * V + j], -g_mean) - h * gh_mean));
+          dw[i * V + j] = __builtin_fmaf(dy, h, dw[i * V + j]);
           db[i * V + j] += dy;
         }
-        if (a.out != nullptr && (kFull || kShort || cols.skip[i] < V))
-          store_row<T, V, kShort>(static_cast<T*>(a.out) + r * a.out_stride, cols.at[i], dim, o);
+        if (a.out != nullptr && (kFull || cols.skip[i] < V))
+          store_row<T, V, false>(static_cast<T*>(a.out) + r * a.out_stride, cols.at[i], dim, o);
       }
     }
   }
   if (a.sums == nullptr) return;
-  float* mine = a.sums + (int64_t)blockIdx.x * 2 * dim;
+  Sum* mine = static_cast<Sum*>(a.sums) + (int64_t)blockIdx.x * 2 * dim;
   if constexpr (kBlock) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
@@ -356,7 +395,7 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
           const Sum* at4 = sums + k * width + at;
           t += ((double)at4[0] + (double)at4[width]) + ((double)at4[2 * width] + (double)at4[3 * width]);
         }
-        mine[which * dim + c] = (float)t;
+        mine[which * dim + c] = (Sum)t;
       }
     }
   }
@@ -366,8 +405,8 @@ __global__ __launch_bounds__(kMost ? kMost : kNormThreads, sizeof(T) == 2 && kMo
 // (of both arrays) a block, a column's sums taken by 64 threads in turn: bound by
 // the latency of their loads, 4 us for 625 blocks' sums of 1021 columns.
 constexpr int kJoinCols = 16, kJoinSlices = 64;
-template <class T>
-__global__ __launch_bounds__(kJoinCols * kJoinSlices) void k_norm_join(const float* sums, int blocks, int dim, void* dw,
+template <class T, class Sum>
+__global__ __launch_bounds__(kJoinCols * kJoinSlices) void k_norm_join(const Sum* sums, int blocks, int dim, void* dw,
                                                                        void* db, bool wide) {
   __shared__ double part[kJoinSlices][kJoinCols];
   const int col = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
@@ -402,7 +441,7 @@ struct NormPlan {
 
 // Blocks that the device holds at a time, and no call has more: a block takes
 // its rows in turn, and its columns of weight and bias once. (Each block of a
-// gradient also leaves 2 * dim floats of sums.)
+// gradient also leaves 2 * dim sums.)
 constexpr int kUnits = 256;
 int blocks_max(const NormPlan& p, bool grad) {
   // waves a unit by the kernels' registers
@@ -531,7 +570,7 @@ int64_t mlkv_layer_norm_grad_workspace(int64_t n, int32_t dim) {
   // (the type is not known here: the most blocks of any)
   int64_t blocks = 0;
   for (int size : {2, 4}) blocks = std::max<int64_t>(blocks, norm_blocks(norm_plan(dim, size), n, true));
-  return (int64_t)sizeof(float) * 2 * dim * blocks;
+  return (int64_t)(dim < 16 / 2 ? sizeof(double) : sizeof(float)) * 2 * dim * blocks;
 }
 
 int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight, const void* d_grad,
@@ -572,7 +611,7 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
     a.grad = d_grad;
     a.weight = d_weight;
     a.out = d_x_grad;
-    a.sums = sums ? static_cast<float*>(d_work) : nullptr;
+    a.sums = sums ? d_work : nullptr;
     a.x_stride = x_stride;
     a.grad_stride = grad_stride;
     a.out_stride = x_grad_stride;
@@ -588,10 +627,14 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   }
   if (!sums) return MLKV_OK;
   const hipError_t e = dispatch_type(dtype, [&](auto t) {
-    hipLaunchKernelGGL((k_norm_join<decltype(t)>), dim3((2 * dim + kJoinCols - 1) / kJoinCols),
-                       dim3(kJoinCols * kJoinSlices), 0, st,
-                       static_cast<const float*>(d_work), blocks, dim, d_weight_grad, d_bias_grad,
-                       weight_dtype == MLKV_F32);
+    const auto join = [&](auto of) {
+      using Sum = decltype(of);
+      hipLaunchKernelGGL((k_norm_join<decltype(t), Sum>), dim3((2 * dim + kJoinCols - 1) / kJoinCols),
+                         dim3(kJoinCols * kJoinSlices), 0, st, static_cast<const Sum*>(d_work), blocks, dim,
+                         d_weight_grad, d_bias_grad, weight_dtype == MLKV_F32);
+    };
+    if (dim < 16 / size) join(double{});
+    else join(float{});
     return hipGetLastError();
   });
   return e == hipSuccess ? MLKV_OK : op_launch_error(e, "mlkv_layer_norm_grad launch");
