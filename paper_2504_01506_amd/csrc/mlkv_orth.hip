@@ -13,7 +13,7 @@
 // is 2^-22 of it, below the rounding of the fp32 sums. Bound by the matrix
 // units: three fp16 products instead of one fp32 product, at 7 times the rate. Five
 // steps of 4096 x 4096 take 4.1 ms, 1.0 PFLOP/s of fp16 products, of which a large
-// library product reaches 1.08 to 1.33, by box.
+// library product reaches 1.08 to 1.33, by card.
 //
 // Updates in bf16 and fp16 take the same pairs: what a step rounds off lies in
 // the directions of small singular values too, and each later step stretches it
