@@ -919,9 +919,9 @@ int mlkv_log_probs_grad(const void* d_logits, int64_t stride, const int64_t* d_t
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (n > 1 && d_logits_grad == d_logits && stride != grad_stride)
     return op_error(MLKV_EINVAL, "logits_grad may be logits only with the same stride");
-  const RowSpan out{d_logits_grad, grad_stride * size, n, vocab * size};
+  const RowSpan out = row_span(d_logits_grad, grad_stride, n, vocab, size);
   const auto meets = [&](const void* p, int64_t bytes) { return rows_meet({p, 0, 1, n * bytes}, out); };
-  if (!out_ok({d_logits, stride * size, n, vocab * size}, out) || meets(d_tokens, 8) || meets(d_stats, 8) ||
+  if (!out_ok(row_span(d_logits, stride, n, vocab, size), out) || meets(d_tokens, 8) || meets(d_stats, 8) ||
       meets(d_entropy, 4) || meets(d_logp_grad, 4) || meets(d_entropy_grad, 4))
     return op_error(MLKV_EINVAL, "logits_grad overlaps an input");
   if (n == 0) return MLKV_OK;

@@ -539,7 +539,7 @@ int mlkv_layer_norm(const void* d_x, int64_t x_stride, const void* d_weight, con
     return op_error(MLKV_EINVAL, "a pointer is not aligned to its element type");
   if (d_out == d_x && n > 1 && x_stride != out_stride)
     return op_error(MLKV_EINVAL, "out may be x only with the same stride");
-  const RowSpan x{d_x, x_stride * size, n, (int64_t)dim * size}, out{d_out, out_stride * size, n, (int64_t)dim * size};
+  const RowSpan x = row_span(d_x, x_stride, n, dim, size), out = row_span(d_out, out_stride, n, dim, size);
   const int64_t params = (int64_t)dim * wsize;
   if (!out_ok(x, out) || rows_meet({d_weight, 0, 1, params}, out) || rows_meet({d_bias, 0, 1, params}, out))
     return op_error(MLKV_EINVAL, "out overlaps x, weight or bias");
@@ -591,9 +591,8 @@ int mlkv_layer_norm_grad(const void* d_x, int64_t x_stride, const void* d_weight
   if (n > 1 && d_x_grad != nullptr &&
       ((d_x_grad == d_x && x_grad_stride != x_stride) || (d_x_grad == d_grad && x_grad_stride != grad_stride)))
     return op_error(MLKV_EINVAL, "x_grad may be x or grad only with the same stride");
-  const int64_t width = (int64_t)dim * size;
-  const RowSpan x{d_x, x_stride * size, n, width}, grad{d_grad, grad_stride * size, n, width},
-      x_grad{d_x_grad, x_grad_stride * size, n, width};
+  const RowSpan x = row_span(d_x, x_stride, n, dim, size), grad = row_span(d_grad, grad_stride, n, dim, size),
+                x_grad = row_span(d_x_grad, x_grad_stride, n, dim, size);
   if (!out_ok(x, x_grad) || !out_ok(grad, x_grad) || rows_meet({d_weight, 0, 1, (int64_t)dim * wsize}, x_grad))
     return op_error(MLKV_EINVAL, "x_grad overlaps x, grad or weight");
   if (sums && n > 0) {

@@ -49,11 +49,16 @@ inline bool stride_ok(int64_t stride, int64_t rows, int64_t width, bool same) {
   return stride >= width && stride <= (int64_t(1) << 60) / rows;
 }
 
-// `rows` rows of `width` bytes, `stride` bytes apart, as stride_ok has passed them.
+// `rows` rows of `width` bytes, `stride` bytes apart.
 struct RowSpan {
   const void* p;
   int64_t stride, rows, width;
 };
+
+// ... of elements of `size` bytes, as stride_ok has passed them (one row's stride may be anything).
+inline RowSpan row_span(const void* p, int64_t stride, int64_t rows, int64_t width, int size) {
+  return {p, rows > 1 ? stride * size : 0, rows, width * size};
+}
 
 // Whether a byte of a's rows is one of b's; b's rows do not overlap each other.
 // Exact, so that rows side by side in one buffer are told apart: at once where
@@ -102,7 +107,7 @@ inline bool rows_meet(RowSpan a, RowSpan b) {
 
 // Whether output rows may lie there: they are the input's own, in place, or share no byte with them.
 inline bool out_ok(const RowSpan& in, const RowSpan& out) {
-  return (in.p == out.p && (in.rows <= 1 || in.stride == out.stride)) || !rows_meet(in, out);
+  return (in.p == out.p && in.stride == out.stride) || !rows_meet(in, out);
 }
 
 // V elements of T as one load or store at any address that T may have: 16

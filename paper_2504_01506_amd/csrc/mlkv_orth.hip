@@ -946,9 +946,13 @@ struct Stack {
   RowSpan one;
   int64_t span() const { return (one.rows - 1) * one.stride + one.width; }
 };
-Stack stack_of(const void* p, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows, int64_t width) {
+Stack stack_of(const void* p, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows, int64_t cols,
+               int size) {
   if (batch <= 1 || batch_stride == 0) batch = 1, batch_stride = 0;
   if (rows <= 1 || row_stride == 0) rows = 1, row_stride = 0;
+  batch_stride *= size;
+  row_stride *= size;
+  const int64_t width = cols * size;
   if (batch > 1 && (rows == 1 || row_stride <= batch_stride))
     return {batch_stride, batch, {p, row_stride, rows, width}};
   return {row_stride, rows, {p, batch_stride, batch, width}};
@@ -1018,8 +1022,8 @@ int mlkv_orthogonalize(const void* d_g, int64_t batch_stride, int64_t row_stride
     return op_error(MLKV_EINVAL, "batch strides must not make matrices overlap");
   if (d_out == d_g && ((rows > 1 && row_stride != out_row_stride) || (batch > 1 && batch_stride != out_batch_stride)))
     return op_error(MLKV_EINVAL, "out may be g only with the same strides");
-  if (d_out != d_g && stacks_meet(stack_of(d_g, batch_stride * size, row_stride * size, batch, rows, cols * size),
-                                  stack_of(d_out, out_batch_stride * size, out_row_stride * size, batch, rows, cols * size)))
+  if (d_out != d_g && stacks_meet(stack_of(d_g, batch_stride, row_stride, batch, rows, cols, size),
+                                  stack_of(d_out, out_batch_stride, out_row_stride, batch, rows, cols, size)))
     return op_error(MLKV_EINVAL, "out overlaps g");
   const Layout l = layout(batch, rows, cols);
   if (l.bytes > 0 && (d_work == nullptr || work_bytes < l.bytes))

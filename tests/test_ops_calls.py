@@ -228,3 +228,12 @@ def test_a_view_that_stands_for_its_negative_is_no_argument():
     x = torch.ones(4)
     with pytest.raises(ValueError, match="resolved"):
         ops._check(torch._neg_view(x), "weight", x)
+
+
+def test_one_rows_stride_may_be_anything():
+    """... and is not multiplied (2^62 elements of 4 bytes would wrap to an overlap of itself)."""
+    far = 2 ** 62
+    assert not rows_call(1000, far, 5000, far, 1) and not rows_call(1000, -far, 1000, far, 1)
+    assert rows_call(1000, far, 1063, -far, 1) and not rows_call(1000, far, 1064, -far, 1)
+    assert "work" in orth(batch=1, gb=far, ob=-far, rows=70) and "overlaps" in orth(batch=1, gb=far, ob=-far, out=4096 + 400)
+    assert "work" in orth(rows=1, gr=far, orow=-far, cols=257, gb=257, ob=257)
